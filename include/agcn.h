@@ -20,7 +20,9 @@
  *
  * and, for a whole GCNConv layer (Sec. II-A), agcn_linear (X W on the matrix
  * cores, no plan needed) and agcn_gcn_layer (linear, then the aggregation
- * with the activation).
+ * with the activation). For inference in 8 bits: agcn_rms_norm,
+ * agcn_quantize_rows, agcn_quantize_weight, agcn_quantized_linear and
+ * agcn_grouped_linear, no plan needed either.
  *
  * Conventions for every call:
  *   - Pointers named d_* are device pointers (memory of the current HIP
@@ -306,6 +308,80 @@ int agcn_gcn_workspace_size(agcn_plan_t plan, int32_t fout, size_t* bytes);
 int agcn_gcn_layer(agcn_plan_t plan, int32_t fin, int32_t fout, const float* d_X, int64_t ldx,
                    const float* d_W, int64_t ldw, float* d_Y, int64_t ldy, void* d_ws,
                    void* stream, int32_t epilogue);
+
+/* ---- 8-bit operators --------------------------------------------------
+ *
+ * The dense half of a deep or typed graph network at inference: rows of a
+ * residual stream are normalised and held in 8 bits, and multiplied by weights
+ * held in 8 bits. A matrix in 8 bits is
+ *   Q  e4m3 values (the OCP 8-bit float with 4 exponent and 3 mantissa bits, no
+ *      infinity, largest value 448), one byte each, row-major;
+ *   S  scales, one byte each (exponent + 127 of a power of two, 255 = NaN): for
+ *      rows one per row and 128 columns, S[row * lds + column / 128]; for a
+ *      weight one per 128 x 128 block, S[(row / 128) * lds + column / 128];
+ * and stands for Q times the scale. The scale of a block is the least 2^e with
+ * e >= -126 that brings its largest finite value to 448 or less; values are
+ * rounded to nearest even after it, infinities and NaN become NaN, and do not
+ * count for the scale.
+ *
+ * Asynchronous on `stream`, without workspace or allocation, so they can be
+ * captured into a graph; results do not depend on timing (no atomics). Any
+ * stride and any alignment to the element is taken; rows of Q that start on 16 bytes
+ * (pointer and stride) are read fastest. Errors: INVALID_ARGUMENT (negative
+ * sizes, strides shorter than a row, NULL pointers with non-empty extents,
+ * outputs that overlap inputs or each other, unknown types), UNSUPPORTED (sizes past a
+ * launch's limits), HIP. */
+
+/* Element types of the 8-bit operators' other matrices. */
+#define AGCN_FLOAT 0  /* 32-bit */
+#define AGCN_BFLOAT 1 /* bfloat16 */
+#define AGCN_HALF 2   /* IEEE 16-bit */
+
+/* The rows of X (n x f, dtype) in 8 bits. */
+int agcn_quantize_rows(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, void* d_Q,
+                       int64_t ldq, void* d_S, int64_t lds, void* stream);
+
+/* Weights W (groups x fin x fout, dtype; rows of fout, as agcn_linear takes
+ * them, group_w elements from one group to the next) in 8 bits, transposed:
+ * d_Q holds fout rows of fin values per group, d_S ceil(fout / 128) rows of
+ * ceil(fin / 128) scales. */
+int agcn_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* d_W,
+                         int64_t ldw, int64_t group_w, void* d_Q, int64_t ldq, int64_t group_q,
+                         void* d_S, int64_t lds, int64_t group_s, void* stream);
+
+/* h = x + r and y = h / sqrt(mean(h^2) + eps) * g per row of f columns, y held in
+ * 8 bits in d_Q and d_S, h in d_H. X, R and H are n x f of `dtype`; R may be
+ * NULL (h = x), H may be NULL, and H may be X or R itself (same pointer and stride).
+ * g: f values of g_dtype, which is dtype or AGCN_FLOAT. Sums and y are
+ * in 32 bits from the unrounded h; a row whose squares overflow 32 bits is summed
+ * scaled. eps > 0 and finite. */
+int agcn_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx,
+                  const void* d_R, int64_t ldr, void* d_H, int64_t ldh, const void* d_g,
+                  int32_t g_dtype, float eps, void* d_Q, int64_t ldq, void* d_S, int64_t lds,
+                  void* stream);
+
+/* Y = epilogue(A W^T), n x fout of `dtype`: A n rows of fin in 8 bits (d_Q,
+ * d_S), W fout rows of fin in 8 bits (d_WQ, d_WS). Sums are in 32 bits. For
+ * AGCN_FLOAT every product is exact and the error that of fp32 sums; for the
+ * 16-bit types the products are added by the 8-bit matrix instruction (error about
+ * 1.5e-5 of the result's 2-norm, below the rounding to the type). fin = 0 gives Y = 0. */
+int agcn_quantized_linear(int64_t n, int32_t fin, int32_t fout, const void* d_Q, int64_t ldq,
+                          const void* d_S, int64_t lds, const void* d_WQ, int64_t ldwq,
+                          const void* d_WS, int64_t ldws, int32_t dtype, void* d_Y, int64_t ldy,
+                          void* stream, int32_t epilogue);
+
+/* The same with a weight per group of rows (expert, node type, relation):
+ * rows d_offsets[e] to d_offsets[e + 1] - 1 take weight e, at group_wq and group_ws
+ * bytes from the one before. d_offsets: groups + 1 device integers that do
+ * not decrease, within [0, n]; groups may be empty, and rows of no group (before the
+ * first offset, from the last on) are set to 0. They are read on the device only.
+ * Offsets that break this leave the rows concerned unspecified, and are never
+ * followed past the matrices. */
+int agcn_grouped_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q,
+                        int64_t ldq, const void* d_S, int64_t lds, const void* d_WQ, int64_t ldwq,
+                        int64_t group_wq, const void* d_WS, int64_t ldws, int64_t group_ws,
+                        const int32_t* d_offsets, int32_t dtype, void* d_Y, int64_t ldy,
+                        void* stream, int32_t epilogue);
 
 /* Fills *out. Host-only, no HIP call. */
 int agcn_plan_info(agcn_plan_t plan, agcn_plan_stats* out);

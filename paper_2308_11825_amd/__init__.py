@@ -19,8 +19,10 @@ __all__ = [
     "agcn_spmm_workspace_size", "agcn_spmm", "agcn_spmm_timed", "agcn_plan_info",
     "agcn_plan_export", "agcn_plan_destroy", "agcn_status_string", "agcn_last_error",
     "agcn_release_cached_memory", "agcn_spmm_ex", "agcn_linear", "agcn_gcn_workspace_size",
-    "agcn_gcn_layer", "agcn_spmm_noalloc", "AGCN_NOALLOC_MAX_WORKSPACE", "Plan", "linear",
-    "PlanParams", "PlanStats", "EXPORTED_SYMBOLS",
+    "agcn_gcn_layer", "agcn_spmm_noalloc", "AGCN_NOALLOC_MAX_WORKSPACE", "agcn_quantize_rows",
+    "agcn_quantize_weight", "agcn_rms_norm", "agcn_quantized_linear", "agcn_grouped_linear",
+    "Plan", "linear", "quantize", "quantize_weight", "rms_norm", "quantized_linear",
+    "grouped_linear", "PlanParams", "PlanStats", "EXPORTED_SYMBOLS",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -31,6 +33,8 @@ EXPORTED_SYMBOLS = [
     "agcn_spmm_timed", "agcn_plan_info", "agcn_plan_export", "agcn_plan_destroy",
     "agcn_status_string", "agcn_last_error", "agcn_release_cached_memory", "agcn_spmm_ex",
     "agcn_linear", "agcn_gcn_workspace_size", "agcn_gcn_layer", "agcn_spmm_noalloc",
+    "agcn_quantize_rows", "agcn_quantize_weight", "agcn_rms_norm", "agcn_quantized_linear",
+    "agcn_grouped_linear",
 ]
 
 AGCN_OK = 0
@@ -47,6 +51,10 @@ AGCN_NOALLOC_MAX_WORKSPACE = 64 << 20
 
 AGCN_EPILOGUE_NONE = 0
 AGCN_EPILOGUE_RELU = 1
+AGCN_FLOAT = 0
+AGCN_BFLOAT = 1
+AGCN_HALF = 2
+
 _EPILOGUES = {None: AGCN_EPILOGUE_NONE, "none": AGCN_EPILOGUE_NONE, "relu": AGCN_EPILOGUE_RELU}
 
 
@@ -142,6 +150,21 @@ def load_library(path: str | None = None):
     lib.agcn_gcn_layer.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
                                    ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, ctypes.c_int32]
     lib.agcn_gcn_layer.restype = ctypes.c_int
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.agcn_quantize_rows.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp]
+    lib.agcn_quantize_rows.restype = ctypes.c_int
+    lib.agcn_quantize_weight.argtypes = [i32, i32, i32, i32, _vp, i64, i64, _vp, i64, i64, _vp, i64,
+                                         i64, _vp]
+    lib.agcn_quantize_weight.restype = ctypes.c_int
+    lib.agcn_rms_norm.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i32,
+                                  ctypes.c_float, _vp, i64, _vp, i64, _vp]
+    lib.agcn_rms_norm.restype = ctypes.c_int
+    lib.agcn_quantized_linear.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i64,
+                                          i32, _vp, i64, _vp, i32]
+    lib.agcn_quantized_linear.restype = ctypes.c_int
+    lib.agcn_grouped_linear.argtypes = [i64, i32, i32, i32, _vp, i64, _vp, i64, _vp, i64, i64, _vp,
+                                        i64, i64, _vp, i32, _vp, i64, _vp, i32]
+    lib.agcn_grouped_linear.restype = ctypes.c_int
     lib.agcn_plan_info.argtypes = [_vp, ctypes.POINTER(PlanStats)]
     lib.agcn_plan_info.restype = ctypes.c_int
     lib.agcn_plan_export.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp]
@@ -217,6 +240,36 @@ def agcn_gcn_workspace_size(plan, fout) -> int:
 def agcn_gcn_layer(plan, fin, fout, d_X, ldx, d_W, ldw, d_Y, ldy, d_ws, stream, epilogue):
     _check(load_library().agcn_gcn_layer(plan, fin, fout, d_X, ldx, d_W, ldw, d_Y, ldy, d_ws,
                                          stream, epilogue))
+
+
+def agcn_quantize_rows(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, lds, stream=0):
+    _check(load_library().agcn_quantize_rows(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, lds, stream))
+
+
+def agcn_quantize_weight(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q, ldq, group_q, d_S, lds,
+                         group_s, stream=0):
+    _check(load_library().agcn_quantize_weight(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q,
+                                               ldq, group_q, d_S, lds, group_s, stream))
+
+
+def agcn_rms_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, g_dtype, eps, d_Q, ldq, d_S, lds,
+                  stream=0):
+    _check(load_library().agcn_rms_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, g_dtype,
+                                        eps, d_Q, ldq, d_S, lds, stream))
+
+
+def agcn_quantized_linear(n, fin, fout, d_Q, ldq, d_S, lds, d_WQ, ldwq, d_WS, ldws, dtype, d_Y, ldy,
+                          stream=0, epilogue=AGCN_EPILOGUE_NONE):
+    _check(load_library().agcn_quantized_linear(n, fin, fout, d_Q, ldq, d_S, lds, d_WQ, ldwq, d_WS,
+                                                ldws, dtype, d_Y, ldy, stream, epilogue))
+
+
+def agcn_grouped_linear(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq, group_wq, d_WS, ldws,
+                        group_ws, d_offsets, dtype, d_Y, ldy, stream=0,
+                        epilogue=AGCN_EPILOGUE_NONE):
+    _check(load_library().agcn_grouped_linear(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq,
+                                              group_wq, d_WS, ldws, group_ws, d_offsets, dtype, d_Y,
+                                              ldy, stream, epilogue))
 
 
 def agcn_plan_info(plan) -> PlanStats:
@@ -453,3 +506,200 @@ def linear(X, W, out=None, stream=None):
     _call(X.device, agcn_linear, n, fin, fout, X.data_ptr(), _row_stride(X), W.data_ptr(),
           _row_stride(W), out.data_ptr(), _row_stride(out), st)
     return out
+
+
+# ---- 8-bit operators ----
+#
+# A matrix in 8 bits is a pair of tensors: the values Q (torch.float8_e4m3fn) and the
+# scales S (torch.float8_e8m0fnu, powers of two), one per 128 columns of a row, or
+# one per 128 x 128 block of a weight. It stands for Q times its scales.
+
+_DTYPES = {}  # torch dtype -> AGCN_FLOAT, AGCN_BFLOAT, AGCN_HALF
+
+
+def _dtype_code(dtype):
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: AGCN_FLOAT, torch.bfloat16: AGCN_BFLOAT,
+                        torch.float16: AGCN_HALF})
+    return _DTYPES.get(dtype)
+
+
+def _check_2d(name, t, device, shape=None, dtype=None, dims=2):
+    """Refuses what is not a matrix (or `dims` - 2 leading axes of them) on `device`
+    with unit column stride, of one of the three types or of `dtype`."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.device != device:
+        raise TypeError(f"{name} must be a CUDA tensor on the inputs' device")
+    if _dtype_code(t.dtype) is None if dtype is None else t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype "
+                        f"{'float32, bfloat16 or float16' if dtype is None else dtype}")
+    if t.dim() != dims or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must have {dims} dimensions"
+                         + ("" if shape is None else f" and shape {shape}"))
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+
+
+def _ld(t):
+    """Row stride of the last two axes (any value >= a row is valid for 0 or 1 rows)."""
+    return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], t.stride(-2))
+
+
+def _on_stream(device, stream, tensors):
+    """The stream's handle; on a stream of the caller's choice torch's allocator must
+    not reuse the tensors' memory before its work."""
+    if stream is None:
+        return _stream_handle(device)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _allocate(device, stream, *shapes):
+    """Tensors of (shape, dtype), allocated on the stream that writes them."""
+    import torch
+    if stream is None:
+        return [torch.empty(s, dtype=d, device=device) for s, d in shapes]
+    with torch.cuda.stream(stream):
+        return [torch.empty(s, dtype=d, device=device) for s, d in shapes]
+
+
+def _allocate_8bit(device, stream, lead, k, scale_rows, *more):
+    """Q (..., k) with rows that start on 16 bytes, and S."""
+    import torch
+    q, s, *rest = _allocate(device, stream, ((*lead, (k + 15) // 16 * 16), torch.float8_e4m3fn),
+                            ((*scale_rows, (k + 127) // 128), torch.float8_e8m0fnu), *more)
+    return (q[..., :k] if k % 16 else q), s, *rest
+
+
+def _check_8bit(names, Q, S, device, lead, k, scale_rows):
+    import torch
+    _check_2d(names[0], Q, device, (*lead, k), torch.float8_e4m3fn, len(lead) + 1)
+    _check_2d(names[1], S, device, (*scale_rows, (k + 127) // 128), torch.float8_e8m0fnu,
+              len(lead) + 1)
+
+
+def quantize(X, out=None, stream=None):
+    """The rows of X (n, f) in 8 bits: (Q, S). X: float32, bfloat16 or float16 CUDA
+    tensor; out: such a pair to write to."""
+    _check_2d("X", X, getattr(X, "device", None))
+    n, f = X.shape
+    if out is None:
+        Q, S = _allocate_8bit(X.device, stream, (n,), f, (n,))
+    else:
+        Q, S = out
+        _check_8bit(("out[0]", "out[1]"), Q, S, X.device, (n,), f, (n,))
+    st = _on_stream(X.device, stream, (X, Q, S))
+    _call(X.device, agcn_quantize_rows, n, f, _dtype_code(X.dtype), X.data_ptr(), _ld(X),
+          Q.data_ptr(), _ld(Q), S.data_ptr(), _ld(S), st)
+    return Q, S
+
+
+def quantize_weight(W, stream=None):
+    """A weight (fin, fout), as ``linear`` takes it, or one per group (groups, fin,
+    fout), in 8 bits for ``quantized_linear`` and ``grouped_linear``: (WQ, WS) with WQ
+    (..., fout, fin), transposed, and WS (..., ceil(fout / 128), ceil(fin / 128))."""
+    dims = W.dim() if hasattr(W, "dim") and W.dim() == 3 else 2
+    _check_2d("W", W, getattr(W, "device", None), dims=dims)
+    *lead, fin, fout = W.shape
+    Q, S = _allocate_8bit(W.device, stream, (*lead, fout), fin, (*lead, (fout + 127) // 128))
+    st = _on_stream(W.device, stream, (W,))
+    groups, strides = (lead[0], [t.stride(0) for t in (W, Q, S)]) if lead else (1, (0, 0, 0))
+    _call(W.device, agcn_quantize_weight, groups, fin, fout, _dtype_code(W.dtype), W.data_ptr(),
+          _ld(W), strides[0], Q.data_ptr(), _ld(Q), strides[1], S.data_ptr(), _ld(S), strides[2],
+          st)
+    return Q, S
+
+
+def rms_norm(X, weight, residual=None, eps=1e-6, hidden=None, out=None, stream=None):
+    """y = h / sqrt(mean(h^2) + eps) * weight per row of h = X + residual, in 8 bits:
+    (Q, S), and with a residual (Q, S, h).
+
+    X, residual and h are (n, f) of one type (float32, bfloat16 or float16), weight (f,)
+    of that type or float32. hidden: where h is written (X or residual itself will
+    do); out: a pair (Q, S) to write to."""
+    _check_2d("X", X, getattr(X, "device", None))
+    n, f = X.shape
+    device, dtype = X.device, X.dtype
+    if weight.dim() != 1 or weight.shape[0] != f or (f > 1 and weight.stride(0) != 1):
+        raise ValueError("weight must be (f,) and contiguous")
+    if weight.device != device or _dtype_code(weight.dtype) not in (AGCN_FLOAT, _dtype_code(dtype)):
+        raise TypeError("weight must be float32 or of X's type, on X's device")
+    if residual is not None:
+        _check_2d("residual", residual, device, (n, f), dtype)
+    elif hidden is not None:
+        raise ValueError("hidden needs a residual: without one h is X")
+    if hidden is not None:
+        _check_2d("hidden", hidden, device, (n, f), dtype)
+    more = [((n, f), dtype)] if residual is not None and hidden is None else []
+    if out is None:
+        Q, S, *new = _allocate_8bit(device, stream, (n,), f, (n,), *more)
+    else:
+        Q, S = out
+        _check_8bit(("out[0]", "out[1]"), Q, S, device, (n,), f, (n,))
+        new = _allocate(device, stream, *more)
+    H = new[0] if new else hidden
+    st = _on_stream(device, stream, (X, weight, residual, H, Q, S))
+    r = (None, 0) if residual is None else (residual.data_ptr(), _ld(residual))
+    h = (None, 0) if H is None else (H.data_ptr(), _ld(H))
+    _call(device, agcn_rms_norm, n, f, _dtype_code(dtype), X.data_ptr(), _ld(X), *r, *h,
+          weight.data_ptr(), _dtype_code(weight.dtype), eps, Q.data_ptr(), _ld(Q), S.data_ptr(),
+          _ld(S), st)
+    return (Q, S) if residual is None else (Q, S, H)
+
+
+def _product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
+    import torch
+    lead = () if offsets is None else (WQ.shape[0],) if getattr(WQ, "dim", int)() == 3 else (0,)
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 2 or not isinstance(WQ, torch.Tensor) or \
+            WQ.dim() != 2 + len(lead):
+        raise ValueError("Q must be (n, fin) and WQ (fout, fin), or (groups, fout, fin) with "
+                         "offsets")
+    n, fin = Q.shape
+    fout = WQ.shape[-2]
+    device, code = Q.device, _dtype_code(torch.float32 if dtype is None else dtype)
+    _check_8bit(("Q", "S"), Q, S, device, (n,), fin, (n,))
+    _check_8bit(("WQ", "WS"), WQ, WS, device, (*lead, fout), fin, (*lead, (fout + 127) // 128))
+    if code is None:
+        raise TypeError("dtype must be float32, bfloat16 or float16")
+    if act not in _EPILOGUES:
+        raise ValueError("act must be None, 'none' or 'relu'")
+    if out is None:
+        out, = _allocate(device, stream, ((n, fout), torch.float32 if dtype is None else dtype))
+    else:
+        _check_2d("out", out, device, (n, fout), out.dtype if dtype is None else dtype)
+        code = _dtype_code(out.dtype)
+        if code is None:
+            raise TypeError("out must be float32, bfloat16 or float16")
+    st = _on_stream(device, stream, (Q, S, WQ, WS, offsets, out))
+    a = (Q.data_ptr(), _ld(Q), S.data_ptr(), _ld(S), WQ.data_ptr(), _ld(WQ))
+    y = (code, out.data_ptr(), _ld(out), st, _EPILOGUES[act])
+    if offsets is None:
+        _call(device, agcn_quantized_linear, n, fin, fout, *a, WS.data_ptr(), _ld(WS), *y)
+        return out
+    if offsets.dtype != torch.int32 or offsets.device != device:
+        raise TypeError("offsets must be int32 on the inputs' device")
+    if tuple(offsets.shape) != (lead[0] + 1,) or (lead[0] > 0 and offsets.stride(0) != 1):
+        raise ValueError("offsets must be (groups + 1,) and contiguous")
+    _call(device, agcn_grouped_linear, n, fin, fout, lead[0], *a, WQ.stride(0), WS.data_ptr(),
+          _ld(WS), WS.stride(0), offsets.data_ptr(), *y)
+    return out
+
+
+def quantized_linear(Q, S, WQ, WS, dtype=None, act=None, out=None, stream=None):
+    """act(A W^T), (n, fout), of A (n, fin) and W (fout, fin) in 8 bits, as ``quantize``
+    or ``rms_norm`` and ``quantize_weight`` give them. dtype: float32 (the default),
+    bfloat16 or float16; act: None or "relu"."""
+    return _product(Q, S, WQ, WS, None, dtype, act, out, stream)
+
+
+def grouped_linear(Q, S, WQ, WS, offsets, dtype=None, act=None, out=None, stream=None):
+    """``quantized_linear`` with a weight per group of rows (expert, node type,
+    relation): rows offsets[e] to offsets[e + 1] - 1 take WQ[e], WS[e]. offsets: int32 CUDA
+    tensor of groups + 1 values that do not decrease, read on the device only; rows
+    of no group are 0."""
+    if offsets is None or not hasattr(offsets, "data_ptr"):
+        raise TypeError("offsets must be an int32 CUDA tensor")
+    return _product(Q, S, WQ, WS, offsets, dtype, act, out, stream)

@@ -739,3 +739,178 @@ int agcn_plan_export(agcn_plan_t plan, int32_t* h_perm, int32_t* h_rowptr_s, int
 void agcn_plan_destroy(agcn_plan_t plan) { plan_free(plan); }
 
 }  // extern "C"
+
+// ---- 8-bit operators -----------------------------------------------------------
+
+namespace {
+
+// One matrix argument: rows x cols elements of `size` bytes, `group` elements
+// between `groups` such matrices.
+struct Matrix {
+  const char* name;
+  const void* p;
+  int64_t rows, cols, ld, size;
+  bool out;
+  int64_t groups = 1, group = 0;
+  size_t bytes = 0;  // its span, set by check_matrices
+};
+
+// Widest matrices of the 8-bit operators (their kernels count columns in 32 bits,
+// and a launch's workgroups along them).
+constexpr int32_t kMostWidth = 1 << 24;
+
+template <size_t N>
+int check_matrices(Matrix (&m)[N]) {
+  for (Matrix& a : m) {
+    const std::string name = a.name;
+    if (a.ld < a.cols) return fail(AGCN_ERR_INVALID_ARGUMENT, name + ": stride shorter than a row");
+    const bool empty = a.rows <= 0 || a.cols <= 0 || a.groups <= 0;
+    if (empty) continue;
+    if (a.rows > 1 && a.ld > (INT64_MAX / 8 - a.cols) / a.rows)
+      return fail(AGCN_ERR_INVALID_ARGUMENT, name + ": matrix extent overflows");
+    const int64_t span = (a.rows - 1) * a.ld + a.cols;
+    if (a.groups > 1) {
+      if (a.group < (a.out ? span : 0))
+        return fail(AGCN_ERR_INVALID_ARGUMENT, name + ": groups overlap, or their stride is negative");
+      if (a.group > (INT64_MAX / 8 - span) / a.groups)
+        return fail(AGCN_ERR_INVALID_ARGUMENT, name + ": matrix extent overflows");
+    }
+    if (a.p == nullptr) return fail(AGCN_ERR_INVALID_ARGUMENT, name + " is NULL");
+    if (a.size > 1 && reinterpret_cast<uintptr_t>(a.p) % (uintptr_t)a.size != 0)
+      return fail(AGCN_ERR_INVALID_ARGUMENT, name + " is not aligned to its elements");
+    a.bytes = (size_t)((span + (a.groups - 1) * a.group) * a.size);
+  }
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j)
+      if (i != j && m[i].out && agcn::ranges_overlap(m[i].p, m[i].bytes, m[j].p, m[j].bytes))
+        return fail(AGCN_ERR_INVALID_ARGUMENT,
+                    std::string(m[i].name) + " overlaps " + m[j].name);
+  return AGCN_OK;
+}
+
+int check_type(int32_t dtype, int64_t* size) {
+  if (dtype != AGCN_FLOAT && dtype != AGCN_BFLOAT && dtype != AGCN_HALF)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "the type must be AGCN_FLOAT, AGCN_BFLOAT or AGCN_HALF");
+  *size = dtype == AGCN_FLOAT ? 4 : 2;
+  return AGCN_OK;
+}
+
+int check_width(int32_t w, const char* name) {
+  if (w < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, std::string(name) + " must be >= 0");
+  if (w > kMostWidth) return fail(AGCN_ERR_UNSUPPORTED, std::string(name) + " is over 2^24");
+  return AGCN_OK;
+}
+
+int64_t q_blocks(int64_t n) { return agcn::ceil_div64(n, 128); }
+
+int quantized_linear_checked(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q,
+                             int64_t ldq, const void* d_S, int64_t lds, const void* d_WQ,
+                             int64_t ldwq, int64_t group_wq, const void* d_WS, int64_t ldws,
+                             int64_t group_ws, const int32_t* d_offsets, bool grouped, int32_t dtype,
+                             void* d_Y, int64_t ldy, void* stream, int32_t epilogue) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(fin, "fin")) return rc;
+  if (int rc = check_width(fout, "fout")) return rc;
+  if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (grouped && (n > INT32_MAX || groups > kMostWidth))
+    return fail(AGCN_ERR_UNSUPPORTED, "over 2^31 - 1 rows or 2^24 groups");
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  if (epilogue != AGCN_EPILOGUE_NONE && epilogue != AGCN_EPILOGUE_RELU)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "epilogue must be AGCN_EPILOGUE_NONE or AGCN_EPILOGUE_RELU");
+  const bool any = n > 0 && fout > 0;  // without rows of Y nothing is read
+  Matrix m[] = {
+      {"Q", d_Q, any ? n : 0, fin, ldq, 1, false},
+      {"S", d_S, any ? n : 0, q_blocks(fin), lds, 1, false},
+      {"WQ", d_WQ, any ? fout : 0, fin, ldwq, 1, false, groups, group_wq},
+      {"WS", d_WS, any ? q_blocks(fout) : 0, q_blocks(fin), ldws, 1, false, groups, group_ws},
+      {"offsets", d_offsets, any && grouped ? 1 : 0, groups + 1, groups + 1, 4, false},
+      {"Y", d_Y, any ? n : 0, fout, ldy, size, true},
+  };
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_quantized_linear(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq, group_wq,
+                                    d_WS, ldws, group_ws, grouped ? d_offsets : nullptr, dtype, d_Y,
+                                    ldy, static_cast<hipStream_t>(stream), epilogue);
+}
+
+}  // namespace
+
+extern "C" {
+
+int agcn_quantize_rows(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, void* d_Q,
+                       int64_t ldq, void* d_S, int64_t lds, void* stream) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  Matrix m[] = {{"X", d_X, n, f, ldx, size, false},
+                {"Q", d_Q, n, f, ldq, 1, true},
+                {"S", d_S, n, q_blocks(f), lds, 1, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_quantize_rows(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, lds,
+                                 static_cast<hipStream_t>(stream));
+}
+
+int agcn_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* d_W,
+                         int64_t ldw, int64_t group_w, void* d_Q, int64_t ldq, int64_t group_q,
+                         void* d_S, int64_t lds, int64_t group_s, void* stream) {
+  if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (int rc = check_width(fin, "fin")) return rc;
+  if (int rc = check_width(fout, "fout")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  Matrix m[] = {{"W", d_W, fin, fout, ldw, size, false, groups, group_w},
+                {"Q", d_Q, fout, fin, ldq, 1, true, groups, group_q},
+                {"S", d_S, q_blocks(fout), q_blocks(fin), lds, 1, true, groups, group_s}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_quantize_weight(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q, ldq, group_q,
+                                   d_S, lds, group_s, static_cast<hipStream_t>(stream));
+}
+
+int agcn_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx,
+                  const void* d_R, int64_t ldr, void* d_H, int64_t ldh, const void* d_g,
+                  int32_t g_dtype, float eps, void* d_Q, int64_t ldq, void* d_S, int64_t lds,
+                  void* stream) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0, g_size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  if (int rc = check_type(g_dtype, &g_size)) return rc;
+  if (g_dtype != dtype && g_dtype != AGCN_FLOAT)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "g must have the rows' type or AGCN_FLOAT");
+  if (!(eps > 0.0f) || eps > 3.0e38f)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "eps must be positive and finite");
+  // H on X or R, row by row, is read before it is written by the same lane.
+  const bool on_x = d_H != nullptr && d_H == d_X && (ldh == ldx || n <= 1);
+  const bool on_r = d_H != nullptr && d_H == d_R && (ldh == ldr || n <= 1);
+  const int64_t rx = on_x ? 0 : n, rr = d_R != nullptr && !on_r ? n : 0, rh = d_H != nullptr ? n : 0;
+  Matrix m[] = {{"X", d_X, rx, f, ldx, size, false},
+                {"R", d_R, rr, f, d_R != nullptr ? ldr : f, size, false},
+                {"H", d_H, rh, f, d_H != nullptr ? ldh : f, size, true},
+                {"g", d_g, n > 0 ? 1 : 0, f, f, g_size, false},
+                {"Q", d_Q, n, f, ldq, 1, true},
+                {"S", d_S, n, q_blocks(f), lds, 1, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_rms_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, g_dtype, eps, d_Q, ldq,
+                            d_S, lds, static_cast<hipStream_t>(stream));
+}
+
+int agcn_quantized_linear(int64_t n, int32_t fin, int32_t fout, const void* d_Q, int64_t ldq,
+                          const void* d_S, int64_t lds, const void* d_WQ, int64_t ldwq,
+                          const void* d_WS, int64_t ldws, int32_t dtype, void* d_Y, int64_t ldy,
+                          void* stream, int32_t epilogue) {
+  return quantized_linear_checked(n, fin, fout, 1, d_Q, ldq, d_S, lds, d_WQ, ldwq, 0, d_WS, ldws, 0,
+                                  nullptr, false, dtype, d_Y, ldy, stream, epilogue);
+}
+
+int agcn_grouped_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q,
+                        int64_t ldq, const void* d_S, int64_t lds, const void* d_WQ, int64_t ldwq,
+                        int64_t group_wq, const void* d_WS, int64_t ldws, int64_t group_ws,
+                        const int32_t* d_offsets, int32_t dtype, void* d_Y, int64_t ldy,
+                        void* stream, int32_t epilogue) {
+  return quantized_linear_checked(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq, group_wq,
+                                  d_WS, ldws, group_ws, d_offsets, true, dtype, d_Y, ldy, stream,
+                                  epilogue);
+}
+
+}  // extern "C"

@@ -184,6 +184,23 @@ double gather_cost(int32_t F, const float* X, int64_t ldx);
 int run_linear(int64_t n, int32_t fin, int32_t fout, const float* X, int64_t ldx, const float* W,
                int64_t ldw, float* H, int64_t ldh, hipStream_t stream, int32_t act);
 
+// Rows and weights in 8 bits (agcn_quant.hip) and their products
+// (agcn_qlinear.hip); dtypes are AGCN_FLOAT, AGCN_BFLOAT or AGCN_HALF. offsets ==
+// nullptr: one weight for all rows.
+int run_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, const void* R,
+                 int64_t ldr, void* H, int64_t ldh, const void* g, int32_t g_dtype, float eps,
+                 void* Q, int64_t ldq, void* S, int64_t lds, hipStream_t st);
+int run_quantize_rows(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, void* Q,
+                      int64_t ldq, void* S, int64_t lds, hipStream_t st);
+int run_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* W,
+                        int64_t ldw, int64_t group_w, void* Q, int64_t ldq, int64_t group_q, void* S,
+                        int64_t lds, int64_t group_s, hipStream_t st);
+int run_quantized_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* A,
+                         int64_t lda, const void* SA, int64_t ldsa, const void* W, int64_t ldw,
+                         int64_t group_w, const void* SW, int64_t ldsw, int64_t group_sw,
+                         const int32_t* offsets, int32_t dtype, void* Y, int64_t ldy, hipStream_t st,
+                         int32_t act);
+
 // agcn_spmm_noalloc's workspace: a fixed device array of this many bytes in
 // agcn_spmm.hip; noalloc_scratch returns its address on `device` (the
 // current device), looked up on the first call for that device.
