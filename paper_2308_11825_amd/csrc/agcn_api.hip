@@ -755,10 +755,6 @@ struct Matrix {
   size_t bytes = 0;  // its span, set by check_matrices
 };
 
-// Widest matrices of the 8-bit operators (their kernels count columns in 32 bits,
-// and a launch's workgroups along them).
-constexpr int32_t kMostWidth = 1 << 24;
-
 template <size_t N>
 int check_matrices(Matrix (&m)[N]) {
   for (Matrix& a : m) {
@@ -797,7 +793,7 @@ int check_type(int32_t dtype, int64_t* size) {
 
 int check_width(int32_t w, const char* name) {
   if (w < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, std::string(name) + " must be >= 0");
-  if (w > kMostWidth) return fail(AGCN_ERR_UNSUPPORTED, std::string(name) + " is over 2^24");
+  if (w > agcn::kMostWidth) return fail(AGCN_ERR_UNSUPPORTED, std::string(name) + " is over 2^24");
   return AGCN_OK;
 }
 
@@ -812,7 +808,7 @@ int quantized_linear_checked(int64_t n, int32_t fin, int32_t fout, int32_t group
   if (int rc = check_width(fin, "fin")) return rc;
   if (int rc = check_width(fout, "fout")) return rc;
   if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
-  if (grouped && (n > INT32_MAX || groups > kMostWidth))
+  if (grouped && (n > INT32_MAX || groups > agcn::kMostWidth))
     return fail(AGCN_ERR_UNSUPPORTED, "over 2^31 - 1 rows or 2^24 groups");
   int64_t size = 0;
   if (int rc = check_type(dtype, &size)) return rc;

@@ -184,6 +184,10 @@ double gather_cost(int32_t F, const float* X, int64_t ldx);
 int run_linear(int64_t n, int32_t fin, int32_t fout, const float* X, int64_t ldx, const float* W,
                int64_t ldw, float* H, int64_t ldh, hipStream_t stream, int32_t act);
 
+// Widest matrices of the 8-bit operators (their kernels count columns in 32 bits,
+// and a launch's workgroups along them).
+constexpr int32_t kMostWidth = 1 << 24;
+
 // Rows and weights in 8 bits (agcn_quant.hip) and their products
 // (agcn_qlinear.hip); dtypes are AGCN_FLOAT, AGCN_BFLOAT or AGCN_HALF. offsets ==
 // nullptr: one weight for all rows.

@@ -17,6 +17,7 @@
 // W's rows are the instruction's rows and A's its columns: a lane then holds
 // four neighbouring outputs of one row of Y, and the scale of one row of A.
 #include <algorithm>
+#include <type_traits>
 
 #include "agcn_quant.hpp"
 
@@ -27,6 +28,7 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
@@ -218,14 +220,464 @@ int launch_thin(const LinearArgs& p, hipStream_t st) {
   return e == hipSuccess ? AGCN_OK : hip_fail(e, "k_qlinear_thin launch");
 }
 
-// Row tiles are a grid's y, 65,535 at most: longer matrices go in pieces.
-template <bool EXACT, class TY>
-int linear_typed(const LinearArgs& p, hipStream_t st) {
-  if (p.offsets != nullptr) {
-    if (most_slots(p.n, p.groups, 64) > 65535)
-      return fail(AGCN_ERR_UNSUPPORTED, "over 65535 tiles of 64 rows");
-    return launch_thin<4, 4, EXACT, TY, true>(p, st);
+// --- tiles through LDS -------------------------------------------------------------
+
+// Workgroup `i` of `total` as the tile that keeps neighbouring tiles on one of the 8
+// XCDs (workgroups go to them in turn), each with its own L2.
+__device__ __forceinline__ uint32_t xcd_tile(uint32_t i, uint32_t total) {
+  const uint32_t q = total / 8, r = total % 8, x = i % 8;
+  return x * q + min(x, r) + i / 8;
+}
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+// A tile of A or W in LDS: ROWS rows of one block of 128 k. Row R's 16-byte piece c
+// lies at position c ^ key(R): eight neighbouring lanes of a fragment then read the
+// eight different positions, so all banks are used once. PERM: the order in which
+// fragments take the rows: 0 as they are, 16 and 32 so that a lane's outputs are
+// neighbours (rows 0-3, 8-11, ... of 32, and rows 0-3, 16-19, 4-7, ... of 32).
+template <int PERM>
+__device__ __forceinline__ int swizzle_key(int row) {
+  return PERM == 0 ? row & 7 : PERM == 16 ? (row & 3) | ((row >> 1) & 4) : (row & 3) | ((row >> 2) & 4);
+}
+
+// The part of a tile that one wave stages: every WAVES-th eight rows, 16 bytes a
+// lane. Rows past `count` are zeros (the buffer's end); their results are not written.
+template <int ROWS, int WAVES, int PERM>
+struct Stage {
+  static constexpr int kSteps = ROWS / 8 / WAVES;
+  // The lane's piece is the same in all its rows.
+  static_assert(ROWS % (8 * WAVES) == 0 && WAVES % 4 == 0, "whole steps of the swizzle's period");
+  const uint8_t* base;
+  uint32_t bytes;  // to the end of the 4 bytes that hold the last row's last value
+  int32_t ld, count, first, piece;
+
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t stride, int rows, int fin, int wave,
+                                       int lane) {
+    base = p;
+    ld = (int32_t)stride;
+    count = rows;
+    bytes = (uint32_t)(rows - 1) * (uint32_t)ld + (((uint32_t)fin + 3) & ~3u);
+    const int row = wave * 8 + lane / 8;
+    piece = ((lane % 8) ^ swizzle_key<PERM>(row)) * 16;
+    first = row * ld + piece;
   }
+  static __device__ __forceinline__ int place(int i, int wave) { return (i * WAVES + wave) * 1024; }
+
+  // Straight into LDS. The whole offset is the lanes', so that the buffer's end bounds it.
+  __device__ __forceinline__ void issue(uint8_t* lds, int k, int wave) const {
+    const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          res, (__attribute__((address_space(3))) void*)(lds + place(i, wave)), 16,
+          first + (i * WAVES * 8 * ld + k), 0, 0, 0);
+  }
+  // Zeros in the lane's own bytes past a row's end, `left` bytes into the last block.
+  __device__ __forceinline__ void mask(uint8_t* lds, int left, int wave, int lane) const {
+    v4i keep;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int b = left - piece - 4 * w;
+      keep[w] = b <= 0 ? 0 : b >= 4 ? -1 : (1 << (8 * b)) - 1;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      v4i* at = reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16);
+      *at &= keep;
+    }
+  }
+  // Through registers, for rows that do not start on 16 bytes.
+  __device__ __forceinline__ void load(v4i (&v)[kSteps], int fin, int k, int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int row = min((i * WAVES + wave) * 8 + lane / 8, count - 1);
+      v[i] = load16(base + row * ld + piece + k, fin - k - piece);
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* lds, const v4i (&v)[kSteps], int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) *reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16) = v[i];
+  }
+};
+
+// The scales of a wave's MT * TILE rows of A for one block: lane r holds those of
+// rows r, TILE + r, ...; 0 past the last row.
+template <int MT, int TILE>
+struct RowScales {
+  const uint8_t* base;
+  uint32_t bytes;
+  int32_t ld, first;
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t stride, int rows, int blocks, int row) {
+    base = p;
+    ld = (int32_t)stride;
+    bytes = (uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)blocks;
+    first = row * ld;
+  }
+  __device__ __forceinline__ void load(uint32_t (&v)[MT], int b) const {
+    const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+      v[t] = __builtin_amdgcn_raw_buffer_load_b8(res, first + (t * TILE * ld + b), 0, 0);
+  }
+};
+
+// The rows and the column tile of this workgroup: bands of group_m row tiles, in each
+// the row tiles of one column tile after another.
+template <int BM, bool GROUPED>
+__device__ __forceinline__ Rows tile_rows(const LinearArgs& p, uint32_t tiles_n, uint32_t group_m,
+                                          uint32_t* tn) {
+  const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x), tiles_m = gridDim.x / tiles_n;
+  const uint32_t band = tile / (group_m * tiles_n), in = tile % (group_m * tiles_n);
+  const uint32_t high = min(group_m, tiles_m - band * group_m);
+  const uint32_t tm = band * group_m + in % high;
+  *tn = in / high;
+  Rows rows;
+  if constexpr (GROUPED) {
+    rows = find_rows<BM>(p, (int)tm);
+    rows.row = __builtin_amdgcn_readfirstlane((int)rows.row);
+    rows.count = __builtin_amdgcn_readfirstlane(rows.count);
+    rows.group = __builtin_amdgcn_readfirstlane(rows.group);
+  } else {
+    rows.row = (int64_t)tm * BM;
+    rows.count = (int32_t)min((int64_t)BM, p.n - rows.row);
+    rows.group = 0;
+  }
+  return rows;
+}
+
+// Writes RUN neighbouring outputs of a row from column n on, of `count` columns.
+template <int RUN, class TY>
+__device__ __forceinline__ void store_run(const float (&v)[RUN], TY* to, int n, int count, int32_t act) {
+  struct alignas(sizeof(TY)) Run {
+    TY e[RUN];
+  } o;
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) o.e[i] = (TY)q_act(v[i], act);
+  if (n + RUN <= count) {
+    store_any(to + n, o);
+  } else {
+#pragma unroll
+    for (int i = 0; i < RUN; ++i)
+      if (n + i < count) to[n + i] = o.e[i];
+  }
+}
+
+// BM x BN outputs per workgroup of WM x WN waves, TM x TN a wave, one block of 128 k
+// at a time: while the waves multiply one block from LDS, the next is on its way
+// into the other half.
+template <int TM, int TN, int WM, int WN, bool EXACT, class TY, bool GROUPED, bool ASYNC>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, uint32_t tiles_n,
+                                                               uint32_t group_m) {
+  constexpr int BM = TM * WM, BN = TN * WN, WAVES = WM * WN, MT = TM / 16, NT = TN / 16;
+  constexpr int PERM = sizeof(TY) == 2 ? 16 : 0;
+  __shared__ __align__(1024) uint8_t lds0[(BM + BN) * kQBlock];
+  __shared__ __align__(1024) uint8_t lds1[(BM + BN) * kQBlock];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, g = lane / 16, wm = wave % WM, wn = wave / WM;
+  uint32_t tn;
+  const Rows rows = tile_rows<BM, GROUPED>(p, tiles_n, group_m, &tn);
+  if (rows.count <= 0) return;
+  const int n0 = (int)tn * BN, count_n = min(BN, p.fout - n0);
+  v4f acc[NT][MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
+  if (blocks > 0) {
+    Stage<BM, WAVES, 0> sa;
+    Stage<BN, WAVES, PERM> sw;
+    sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, wave, lane);
+    sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, count_n, p.fin, wave, lane);
+    RowScales<MT, 16> scale_a;
+    scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * TM + r);
+    const uint8_t* scale_w =
+        p.SW + rows.group * p.group_sw +
+        (int64_t)min((n0 + wn * TN) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
+    // Fragments: row r of the tile, pieces g and g + 4.
+    const int frag_a = (wm * TM + r) * kQBlock + ((g ^ (r & 7)) * 16);
+    const int frag_w = BM * kQBlock + (wn * TN + (PERM ? 8 * (r / 4) + r % 4 : r)) * kQBlock +
+                       ((g ^ (r & 7)) * 16);
+
+    v4i pre_a[Stage<BM, WAVES, 0>::kSteps], pre_w[Stage<BN, WAVES, PERM>::kSteps];
+    uint32_t code_a[MT], next_a[MT], code_w, next_w = 0;
+    auto fetch = [&](uint8_t* to, int b) {
+      scale_a.load(next_a, b);
+      next_w = scale_w[b];
+      if constexpr (ASYNC) {
+        sa.issue(to, b * kQBlock, wave);
+        sw.issue(to + BM * kQBlock, b * kQBlock, wave);
+      } else {
+        sa.load(pre_a, p.fin, b * kQBlock, wave, lane);
+        sw.load(pre_w, p.fin, b * kQBlock, wave, lane);
+      }
+    };
+    auto arrive = [&](uint8_t* to, int b) {
+      if constexpr (ASYNC) {
+        __builtin_amdgcn_s_waitcnt(0);
+        const int left = p.fin - b * kQBlock;
+        if (left < kQBlock) {
+          sa.mask(to, left, wave, lane);
+          sw.mask(to + BM * kQBlock, left, wave, lane);
+        }
+      } else {
+        sa.store(to, pre_a, wave, lane);
+        sw.store(to + BM * kQBlock, pre_w, wave, lane);
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) code_a[t] = next_a[t];
+      code_w = next_w;
+      __syncthreads();
+    };
+    auto multiply = [&](const uint8_t* lds) {
+      v8i a[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const uint8_t* at = lds + frag_a + t * 16 * kQBlock;
+        a[t] = join(*reinterpret_cast<const v4i*>(at),
+                    *reinterpret_cast<const v4i*>(lds + ((frag_a + t * 16 * kQBlock) ^ 64)));
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int row = PERM ? j / 2 * 32 + j % 2 * 4 : j * 16;
+        const int at = frag_w + row * kQBlock;
+        const v8i w = join(*reinterpret_cast<const v4i*>(lds + at),
+                           *reinterpret_cast<const v4i*>(lds + (at ^ 64)));
+#pragma unroll
+        for (int t = 0; t < MT; ++t) block_product<EXACT>(acc[j][t], w, a[t], code_w, code_a[t]);
+      }
+    };
+    fetch(lds0, 0);
+    arrive(lds0, 0);
+    for (int b = 0; b < blocks; b += 2) {
+      if (b + 1 < blocks) fetch(lds1, b + 1);
+      multiply(lds0);
+      if (b + 1 >= blocks) break;
+      arrive(lds1, b + 1);
+      if (b + 2 < blocks) fetch(lds0, b + 2);
+      multiply(lds1);
+      if (b + 2 < blocks) arrive(lds0, b + 2);
+    }
+  }
+
+  TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
+  constexpr int kRun = PERM ? 8 : 4;  // neighbouring outputs of a lane
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int m = wm * TM + t * 16 + r;
+    if (m >= rows.count) continue;
+#pragma unroll
+    for (int j = 0; j < NT; j += kRun / 4) {
+      float v[kRun];
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) v[i] = acc[j + i / 4][t][i % 4];
+      store_run(v, y + m * p.ldy, wn * TN + (PERM ? j / 2 * 32 + 8 * g : j * 16 + 4 * g), count_n, p.act);
+    }
+  }
+}
+
+// 256 x 256 outputs per workgroup of 4 waves, 128 x 128 a wave: the accumulators fill
+// half of the registers and one wave a SIMD is left, so nothing but the order of its
+// own instructions hides LDS. A block of 128 k is multiplied in four quarters of 64 x 64;
+// each quarter needs only one new half of A or W, which is read from LDS during the
+// quarter before, the first two of the next block among them:
+//   A0 W0 | read W1,   A0 W1 | read A1,   barrier: the next block is in LDS,
+//   A1 W1 | read A0',  A1 W0 | read W1'   and the block after it is on its way.
+template <class TY, bool GROUPED>
+__global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t tiles_n,
+                                                        uint32_t group_m) {
+  constexpr int BM = 256, BN = 256, WAVES = 4;
+  __shared__ __align__(1024) uint8_t lds0[(BM + BN) * kQBlock];
+  __shared__ __align__(1024) uint8_t lds1[(BM + BN) * kQBlock];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 32, g = lane / 32, wm = wave % 2, wn = wave / 2;
+  uint32_t tn;
+  const Rows rows = tile_rows<BM, GROUPED>(p, tiles_n, group_m, &tn);
+  if (rows.count <= 0) return;
+  const int n0 = (int)tn * BN, count_n = min(BN, p.fout - n0);
+  v16f acc[4][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[j][t][i] = 0.0f;
+
+  const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
+  if (blocks > 0) {
+    Stage<BM, WAVES, 0> sa;
+    Stage<BN, WAVES, 32> sw;
+    sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, wave, lane);
+    sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, count_n, p.fin, wave, lane);
+    RowScales<4, 32> scale_a;
+    scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * 128 + r);
+    const uint8_t* scale_w =
+        p.SW + rows.group * p.group_sw +
+        (int64_t)min((n0 + wn * 128) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
+    // Fragments: pieces g, g + 2 (the first 64 k), g + 4 and g + 6 of a row.
+    const int row_w = 16 * (r / 4 % 2) + 4 * (r / 8) + r % 4;
+    const int frag_a = (wm * 128 + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
+    const int frag_w = BM * kQBlock + (wn * 128 + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
+
+    // Two blocks a round; an odd number starts with one of zeros, so that the last
+    // block, which may be a part of one, always comes second in the last round.
+    const int none = blocks & 1, total = blocks + none;
+    uint32_t code_a[4], next_a[4], code_w, next_w;
+    auto issue = [&](uint8_t* to, int i) {
+      sa.issue(to, (i - none) * kQBlock, wave);
+      sw.issue(to + BM * kQBlock, (i - none) * kQBlock, wave);
+    };
+    auto codes = [&](int i) {
+      scale_a.load(next_a, max(i - none, 0));
+      next_w = scale_w[max(i - none, 0)];
+    };
+    auto mask = [&](uint8_t* to, int left) {
+      sa.mask(to, left, wave, lane);
+      sw.mask(to + BM * kQBlock, left, wave, lane);
+    };
+    v8i a0[2][2], a1[2][2], w0[2][2], w1[2][2];  // [tile of 32 rows][half of the block]
+    auto read = [&](v8i (&v)[2][2], const uint8_t* lds, int at) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int x = at + t * 32 * kQBlock;
+          v[t][h] = join(*reinterpret_cast<const v4i*>(lds + (x ^ (64 * h))),
+                         *reinterpret_cast<const v4i*>(lds + (x ^ (64 * h + 32))));
+        }
+    };
+    auto multiply = [&](const v8i (&w)[2][2], const v8i (&a)[2][2], int hw, int ha) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            acc[hw * 2 + j][ha * 2 + t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                w[j][h], a[t][h], acc[hw * 2 + j][ha * 2 + t], 0, 0, 0, (int)code_w, 0,
+                (int)code_a[ha * 2 + t]);
+    };
+    // Block i of `now`, its halves of W in wf and wo (first, other). PART: i + 1 is
+    // the last block; LAST: i is.
+    constexpr int kHalf = 64 * kQBlock;
+    auto step = [&](uint8_t* now, uint8_t* next, int i, int first, v8i (&wf)[2][2], v8i (&wo)[2][2],
+                    auto part, auto end) {
+      constexpr bool PART = decltype(part)::value, LAST = decltype(end)::value;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) code_a[t] = next_a[t];
+      code_w = next_w;
+      read(wo, now, frag_w + (1 - first) * kHalf);
+      if (!LAST) codes(i + 1);
+      multiply(wf, a0, first, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      read(a1, now, frag_a + kHalf);
+      multiply(wo, a0, 1 - first, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!LAST) {
+        __builtin_amdgcn_s_waitcnt(0);
+        if (PART) mask(next, p.fin - (i + 1 - none) * kQBlock);
+        __syncthreads();
+        if (!PART) issue(now, i + 2);
+        read(a0, next, frag_a);
+      }
+      multiply(wo, a1, 1 - first, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!LAST) read(wo, next, frag_w + (1 - first) * kHalf);
+      multiply(wf, a1, first, 1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if (none) mask(lds0, 0);
+    else issue(lds0, 0);
+    codes(0);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    issue(lds1, 1);
+    read(a0, lds0, frag_a);
+    read(w0, lds0, frag_w);
+    int i = 0;
+    for (; i + 2 < total; i += 2) {
+      step(lds0, lds1, i, 0, w0, w1, No{}, No{});
+      step(lds1, lds0, i + 1, 1, w1, w0, No{}, No{});
+    }
+    step(lds0, lds1, i, 0, w0, w1, Yes{}, No{});
+    step(lds1, lds0, i + 1, 1, w1, w0, No{}, Yes{});
+  }
+  TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int m = wm * 128 + t * 32 + r;
+    if (m >= rows.count) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = acc[j][t][8 * h + i];
+        store_run<8>(v, y + m * p.ldy, wn * 128 + j * 32 + 16 * g + 8 * h, count_n, p.act);
+      }
+  }
+}
+
+// Grid of a launch over BM x BN tiles; rows of a band: square patches of about 32
+// tiles, what the 32 CUs of an XCD work on at a time.
+struct TileGrid {
+  int64_t tiles, tiles_n, group_m;
+};
+template <int BM, int BN, bool GROUPED>
+TileGrid tile_grid(const LinearArgs& p) {
+  const int64_t tiles_m = GROUPED ? most_slots(p.n, p.groups, BM) : ceil_div64(p.n, BM);
+  const int64_t tiles_n = ceil_div64(p.fout, BN);
+  return {tiles_m * tiles_n, tiles_n, std::min<int64_t>(tiles_m, 8)};
+}
+constexpr int64_t kMostTiles = INT32_MAX / 256;
+
+int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? AGCN_OK : hip_fail(e, what);
+}
+
+template <int TM, int TN, int WM, int WN, bool EXACT, class TY, bool GROUPED, bool ASYNC>
+int launch_tile(const LinearArgs& p, hipStream_t st) {
+  const TileGrid t = tile_grid<TM * WM, TN * WN, GROUPED>(p);
+  if (t.tiles > kMostTiles) return fail(AGCN_ERR_UNSUPPORTED, "matrix too large for one launch");
+  k_qlinear_tile<TM, TN, WM, WN, EXACT, TY, GROUPED, ASYNC>
+      <<<(unsigned)t.tiles, 64 * WM * WN, 0, st>>>(p, (uint32_t)t.tiles_n, (uint32_t)t.group_m);
+  return launched("k_qlinear_tile launch");
+}
+
+template <class TY, bool GROUPED>
+int launch_big(const LinearArgs& p, hipStream_t st) {
+  const TileGrid t = tile_grid<256, 256, GROUPED>(p);
+  if (t.tiles > kMostTiles) return fail(AGCN_ERR_UNSUPPORTED, "matrix too large for one launch");
+  k_qlinear_big<TY, GROUPED>
+      <<<(unsigned)t.tiles, 256, 0, st>>>(p, (uint32_t)t.tiles_n, (uint32_t)t.group_m);
+  return launched("k_qlinear_big launch");
+}
+
+template <bool EXACT, class TY, bool GROUPED>
+int linear_typed(const LinearArgs& p, hipStream_t st) {
+  const bool async = aligned16(p.A) && aligned16(p.W) && p.lda % 16 == 0 && p.ldw % 16 == 0 &&
+                     p.group_w % 16 == 0;
+  // Offsets inside a tile are 32-bit.
+  const bool near = std::max({p.lda, p.ldw, p.ldsa}) <= (INT32_MAX - kMostWidth) / 256;
+  if (near && p.n > 64) {
+    if constexpr (!EXACT)
+      if (async && p.n >= 256) return launch_big<TY, GROUPED>(p, st);
+    if (async) return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, true>(p, st);
+    return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, false>(p, st);
+  }
+  return launch_thin<4, 4, EXACT, TY, GROUPED>(p, st);
+}
+
+template <bool EXACT, class TY>
+int linear_pieces(const LinearArgs& p, hipStream_t st) {
+  if (p.offsets != nullptr) return linear_typed<EXACT, TY, true>(p, st);
+  // A launch's row tiles: longer matrices go in pieces.
   constexpr int64_t kMost = 65535 * 64;
   for (int64_t r = 0; r < p.n; r += kMost) {
     LinearArgs q = p;
@@ -233,7 +685,7 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
     q.A += r * p.lda;
     q.SA += r * p.ldsa;
     q.Y = static_cast<TY*>(p.Y) + r * p.ldy;
-    if (int rc = launch_thin<4, 4, EXACT, TY, false>(q, st)) return rc;
+    if (int rc = linear_typed<EXACT, TY, false>(q, st)) return rc;
   }
   return AGCN_OK;
 }
@@ -250,9 +702,9 @@ int run_quantized_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, c
                      static_cast<const uint8_t*>(SA), ldsa, static_cast<const uint8_t*>(W), ldw,
                      group_w, static_cast<const uint8_t*>(SW), ldsw, group_sw, offsets, groups, Y,
                      ldy, act};
-  if (dtype == AGCN_FLOAT) return linear_typed<true, float>(p, st);
-  if (dtype == AGCN_BFLOAT) return linear_typed<false, bf16_t>(p, st);
-  return linear_typed<false, f16_t>(p, st);
+  if (dtype == AGCN_FLOAT) return linear_pieces<true, float>(p, st);
+  if (dtype == AGCN_BFLOAT) return linear_pieces<false, bf16_t>(p, st);
+  return linear_pieces<false, f16_t>(p, st);
 }
 
 }  // namespace agcn
