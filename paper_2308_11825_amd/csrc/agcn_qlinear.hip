@@ -231,14 +231,26 @@ __device__ __forceinline__ uint32_t xcd_tile(uint32_t i, uint32_t total) {
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
-// A tile of A or W in LDS: ROWS rows of one block of 128 k. Row R's 16-byte piece c
-// lies at position c ^ key(R): eight neighbouring lanes of a fragment then read the
-// eight different positions, so all banks are used once. PERM: the order in which
-// fragments take the rows: 0 as they are, 16 and 32 so that a lane's outputs are
-// neighbours (rows 0-3, 8-11, ... of 32, and rows 0-3, 16-19, 4-7, ... of 32).
+// A tile of A or W in LDS: rows of one block of 128 k, 128 bytes. Row R's 16-byte
+// piece c lies at position c ^ key(R). LDS has 64 banks, two rows, and serves 16 lanes'
+// 16 bytes at a time: the 16 rows of a fragment that go together take all 16 places of
+// two rows. PERM: the order in which fragments take the rows of W, so that a lane's
+// outputs are neighbours: 0 as they are, 16 rows 0-3, 8-11, 16-19, 24-27 and then 4-7, ...
+// of 32 for two fragments of 16, 32 rows 0-3, 8-11, 4-7, 12-15, 16-19, ... for one of 32.
 template <int PERM>
 __device__ __forceinline__ int swizzle_key(int row) {
-  return PERM == 0 ? row & 7 : PERM == 16 ? (row & 3) | ((row >> 1) & 4) : (row & 3) | ((row >> 2) & 4);
+  return PERM == 16 ? (row >> 1 & 1) | (row >> 2 & 6) : row >> 1 & 7;
+}
+
+// Ones in the first `valid` of 16 bytes.
+__device__ __forceinline__ v4i bytes_kept(int valid) {
+  v4i keep;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int b = valid - 4 * w;
+    keep[w] = b <= 0 ? 0 : b >= 4 ? -1 : (1 << (8 * b)) - 1;
+  }
+  return keep;
 }
 
 // The part of a tile that one wave stages: every WAVES-th eight rows, 16 bytes a
@@ -275,17 +287,10 @@ struct Stage {
   }
   // Zeros in the lane's own bytes past a row's end, `left` bytes into the last block.
   __device__ __forceinline__ void mask(uint8_t* lds, int left, int wave, int lane) const {
-    v4i keep;
+    const v4i keep = bytes_kept(left - piece);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int b = left - piece - 4 * w;
-      keep[w] = b <= 0 ? 0 : b >= 4 ? -1 : (1 << (8 * b)) - 1;
-    }
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      v4i* at = reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16);
-      *at &= keep;
-    }
+    for (int i = 0; i < kSteps; ++i)
+      *reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16) &= keep;
   }
   // Through registers, for rows that do not start on 16 bytes.
   __device__ __forceinline__ void load(v4i (&v)[kSteps], int fin, int k, int wave, int lane) const {
@@ -301,9 +306,38 @@ struct Stage {
   }
 };
 
+// Half of a 256-row tile for 4 waves: of every 128 rows those of half `h`.
+template <int PERM>
+struct HalfStage {
+  const uint8_t* base;
+  uint32_t bytes, first;
+  int32_t ld, piece;
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t stride, int rows, int fin, int wave,
+                                       int lane) {
+    base = p;
+    ld = (int32_t)stride;
+    bytes = (uint32_t)(rows - 1) * (uint32_t)ld + (((uint32_t)fin + 3) & ~3u);
+    const int row = wave * 8 + lane / 8;
+    piece = ((lane % 8) ^ swizzle_key<PERM>(row)) * 16;
+    first = (uint32_t)(row * ld + piece);
+  }
+  static __device__ __forceinline__ int place(int i, int wave) { return (i * 4 + wave) * 1024; }
+  __device__ __forceinline__ void issue(uint8_t* lds, uint32_t k, int h, int i, int wave) const {
+    const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        res, (__attribute__((address_space(3))) void*)(lds + place(i, wave)), 16,
+        first + ((uint32_t)((i / 2 * 128 + i % 2 * 32 + h * 64) * ld) + k), 0, 0, 0);
+  }
+  __device__ __forceinline__ void mask(uint8_t* lds, int left, int wave, int lane) const {
+    const v4i keep = bytes_kept(left - piece);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16) &= keep;
+  }
+};
+
 // The scales of a wave's MT * TILE rows of A for one block: lane r holds those of
 // rows r, TILE + r, ...; 0 past the last row.
-template <int MT, int TILE>
+template <int TILE>
 struct RowScales {
   const uint8_t* base;
   uint32_t bytes;
@@ -314,11 +348,9 @@ struct RowScales {
     bytes = (uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)blocks;
     first = row * ld;
   }
-  __device__ __forceinline__ void load(uint32_t (&v)[MT], int b) const {
+  __device__ __forceinline__ uint32_t load(int t, int b) const {
     const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-      v[t] = __builtin_amdgcn_raw_buffer_load_b8(res, first + (t * TILE * ld + b), 0, 0);
+    return __builtin_amdgcn_raw_buffer_load_b8(res, first + (t * TILE * ld + b), 0, 0);
   }
 };
 
@@ -391,20 +423,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
     Stage<BN, WAVES, PERM> sw;
     sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, wave, lane);
     sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, count_n, p.fin, wave, lane);
-    RowScales<MT, 16> scale_a;
+    RowScales<16> scale_a;
     scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * TM + r);
     const uint8_t* scale_w =
         p.SW + rows.group * p.group_sw +
         (int64_t)min((n0 + wn * TN) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
     // Fragments: row r of the tile, pieces g and g + 4.
-    const int frag_a = (wm * TM + r) * kQBlock + ((g ^ (r & 7)) * 16);
-    const int frag_w = BM * kQBlock + (wn * TN + (PERM ? 8 * (r / 4) + r % 4 : r)) * kQBlock +
-                       ((g ^ (r & 7)) * 16);
+    const int row_w = PERM ? 8 * (r / 4) + r % 4 : r;
+    const int frag_a = (wm * TM + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
+    const int frag_w = BM * kQBlock + (wn * TN + row_w) * kQBlock + ((g ^ swizzle_key<PERM>(row_w)) * 16);
 
     v4i pre_a[Stage<BM, WAVES, 0>::kSteps], pre_w[Stage<BN, WAVES, PERM>::kSteps];
     uint32_t code_a[MT], next_a[MT], code_w, next_w = 0;
     auto fetch = [&](uint8_t* to, int b) {
-      scale_a.load(next_a, b);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) next_a[t] = scale_a.load(t, b);
       next_w = scale_w[b];
       if constexpr (ASYNC) {
         sa.issue(to, b * kQBlock, wave);
@@ -480,17 +513,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
 
 // 256 x 256 outputs per workgroup of 4 waves, 128 x 128 a wave: the accumulators fill
 // half of the registers and one wave a SIMD is left, so nothing but the order of its
-// own instructions hides LDS. A block of 128 k is multiplied in four quarters of 64 x 64;
-// each quarter needs only one new half of A or W, which is read from LDS during the
-// quarter before, the first two of the next block among them:
-//   A0 W0 | read W1,   A0 W1 | read A1,   barrier: the next block is in LDS,
-//   A1 W1 | read A0',  A1 W0 | read W1'   and the block after it is on its way.
+// own instructions hides LDS and memory. A block of 128 k is multiplied in four
+// quarters of 64 x 64, and a quarter needs one new half of A or W, which is read from LDS
+// during the quarter before:
+//   A0 W0 | read W1,   A0 W1 | read A1,   A1 W1 | read A0',   A1 W0 | read W1'
+// (' the next block, which starts with the other half of W). So LDS is filled and
+// emptied in halves of a block, of A and of W together: five slots of 32 KB, one being
+// read and four on their way, which are two blocks' time to arrive.
 template <class TY, bool GROUPED>
 __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t tiles_n,
                                                         uint32_t group_m) {
-  constexpr int BM = 256, BN = 256, WAVES = 4;
-  __shared__ __align__(1024) uint8_t lds0[(BM + BN) * kQBlock];
-  __shared__ __align__(1024) uint8_t lds1[(BM + BN) * kQBlock];
+  constexpr int BM = 256, BN = 256, kSlots = 5, kSlot = 256 * kQBlock, kPart = 128 * kQBlock;
+  __shared__ __align__(1024) uint8_t lds[kSlots * kSlot];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 32, g = lane / 32, wm = wave % 2, wn = wave / 2;
   uint32_t tn;
@@ -507,104 +541,136 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
 
   const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
   if (blocks > 0) {
-    Stage<BM, WAVES, 0> sa;
-    Stage<BN, WAVES, 32> sw;
+    // Two blocks a round; an odd number starts with one of zeros, so that the last
+    // block, which may be a part of one, always comes second in the last round.
+    const int none = blocks & 1, total = blocks + none;
+    HalfStage<0> sa;
+    HalfStage<32> sw;
     sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, wave, lane);
     sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, count_n, p.fin, wave, lane);
-    RowScales<4, 32> scale_a;
+    RowScales<32> scale_a;
     scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * 128 + r);
     const uint8_t* scale_w =
         p.SW + rows.group * p.group_sw +
         (int64_t)min((n0 + wn * 128) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
     // Fragments: pieces g, g + 2 (the first 64 k), g + 4 and g + 6 of a row.
-    const int row_w = 16 * (r / 4 % 2) + 4 * (r / 8) + r % 4;
-    const int frag_a = (wm * 128 + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
-    const int frag_w = BM * kQBlock + (wn * 128 + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
+    const int row_w = r / 16 * 16 + r / 4 % 2 * 8 + r / 8 % 2 * 4 + r % 4;
+    const int frag_a = (wm * 64 + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
+    const int frag_w = kPart + (wn * 64 + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
 
-    // Two blocks a round; an odd number starts with one of zeros, so that the last
-    // block, which may be a part of one, always comes second in the last round.
-    const int none = blocks & 1, total = blocks + none;
     uint32_t code_a[4], next_a[4], code_w, next_w;
-    auto issue = [&](uint8_t* to, int i) {
-      sa.issue(to, (i - none) * kQBlock, wave);
-      sw.issue(to + BM * kQBlock, (i - none) * kQBlock, wave);
+    int to = 0, from = 0;  // slots to fill and to read next
+    auto advance = [](int& slot) { slot = slot == (kSlots - 1) * kSlot ? 0 : slot + kSlot; };
+    // Half h of block i: rows 64 h to 64 h + 63 of every 128 of A, and of W the other
+    // half in odd blocks. Past the last block nothing is read (zeros arrive).
+    // Load l of a wave's 8.
+    auto issue = [&](int i, int h, int l) {
+      const uint32_t k = i < total ? (uint32_t)((i - none) * kQBlock) : 0x80000000u;
+      if (l < 4) sa.issue(lds + to, k, h, l, wave);
+      else sw.issue(lds + to + kPart, k, h ^ (i & 1), l - 4, wave);
+      if (l == 7) advance(to);
     };
-    auto codes = [&](int i) {
-      scale_a.load(next_a, max(i - none, 0));
-      next_w = scale_w[max(i - none, 0)];
+    auto issue_all = [&](int i, int h) {
+#pragma unroll
+      for (int l = 0; l < 8; ++l) issue(i, h, l);
     };
-    auto mask = [&](uint8_t* to, int left) {
-      sa.mask(to, left, wave, lane);
-      sw.mask(to + BM * kQBlock, left, wave, lane);
+    auto code = [&](int i, int l) {
+      const int b = max(i - none, 0);
+      if (l < 4) next_a[l] = scale_a.load(l, b);
+      else next_w = scale_w[b];
     };
-    v8i a0[2][2], a1[2][2], w0[2][2], w1[2][2];  // [tile of 32 rows][half of the block]
-    auto read = [&](v8i (&v)[2][2], const uint8_t* lds, int at) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int x = at + t * 32 * kQBlock;
-          v[t][h] = join(*reinterpret_cast<const v4i*>(lds + (x ^ (64 * h))),
-                         *reinterpret_cast<const v4i*>(lds + (x ^ (64 * h + 32))));
-        }
+    auto mask = [&](int slot, int left) {
+      sa.mask(lds + slot, left, wave, lane);
+      sw.mask(lds + slot + kPart, left, wave, lane);
     };
-    auto multiply = [&](const v8i (&w)[2][2], const v8i (&a)[2][2], int hw, int ha) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            acc[hw * 2 + j][ha * 2 + t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                w[j][h], a[t][h], acc[hw * 2 + j][ha * 2 + t], 0, 0, 0, (int)code_w, 0,
-                (int)code_a[ha * 2 + t]);
+    // The half at `from` is in LDS and the one before it has been read, by all waves.
+    // A half is 8 loads a wave, and three younger ones may be on their way.
+    auto arrive = [&](int left) {
+      asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+      if (left < kQBlock) mask(from, left);
+      // (A fence would wait for every load into LDS.)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
-    // Block i of `now`, its halves of W in wf and wo (first, other). PART: i + 1 is
-    // the last block; LAST: i is.
-    constexpr int kHalf = 64 * kQBlock;
-    auto step = [&](uint8_t* now, uint8_t* next, int i, int first, v8i (&wf)[2][2], v8i (&wo)[2][2],
-                    auto part, auto end) {
-      constexpr bool PART = decltype(part)::value, LAST = decltype(end)::value;
+    v8i a0[4], a1[4], w0[4], w1[4];  // 2 * half of 64 k + tile of 32 rows
+    auto read = [&](v8i (&v)[4], int at, int c) {
+      const int x = at + c % 2 * 32 * kQBlock, h = c / 2 * 64;
+      v[c] = join(*reinterpret_cast<const v4i*>(lds + from + (x ^ h)),
+                  *reinterpret_cast<const v4i*>(lds + from + (x ^ (h + 32))));
+    };
+    // A quarter: eight products, and after the k-th what `between` issues in its shadow.
+    auto quarter = [&](const v8i (&w)[4], const v8i (&a)[4], int hw, int ha, auto between) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int h = k / 4, j = k / 2 % 2, t = k % 2;
+        v16f& c = acc[hw * 2 + j][ha * 2 + t];
+        c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[2 * h + j], a[2 * h + t], c, 0, 0, 0,
+                                                            (int)code_w, 0, (int)code_a[ha * 2 + t]);
+        between(k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // Block i, its first half of W (number `first`) in wf; the other goes to wo. WHICH: 0 a
+    // block in the middle, 1 the one before the last, 2 the last.
+    auto step = [&](int i, int first, v8i (&wf)[4], v8i (&wo)[4], auto which) {
+      constexpr int WHICH = decltype(which)::value;
+      const int left = WHICH == 0 ? kQBlock : p.fin - (blocks - 1) * kQBlock;
 #pragma unroll
       for (int t = 0; t < 4; ++t) code_a[t] = next_a[t];
       code_w = next_w;
-      read(wo, now, frag_w + (1 - first) * kHalf);
-      if (!LAST) codes(i + 1);
-      multiply(wf, a0, first, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      read(a1, now, frag_a + kHalf);
-      multiply(wo, a0, 1 - first, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (!LAST) {
-        __builtin_amdgcn_s_waitcnt(0);
-        if (PART) mask(next, p.fin - (i + 1 - none) * kQBlock);
-        __syncthreads();
-        if (!PART) issue(now, i + 2);
-        read(a0, next, frag_a);
-      }
-      multiply(wo, a1, 1 - first, 1);
-      __builtin_amdgcn_sched_barrier(0);
-      if (!LAST) read(wo, next, frag_w + (1 - first) * kHalf);
-      multiply(wf, a1, first, 1);
-      __builtin_amdgcn_sched_barrier(0);
+      // At most one load after a product: the four waves' loads are taken in turn.
+      quarter(wf, a0, first, 0, [&](int k) {
+        if (k == 0) arrive(WHICH == 2 ? left : kQBlock);
+        else if (k <= 4) read(wo, frag_w, k - 1);
+        if (WHICH == 2) return;
+        if (k >= 1 && k < 6) code(i + 1, k - 1);
+        if (k >= 6) issue(i + 2, 1, k - 6);
+      });
+      quarter(wo, a0, 1 - first, 0, [&](int k) {
+        if (k < 4) read(a1, frag_a, k);
+        if (k == 4) advance(from);
+        if (k >= 2 && WHICH < 2) issue(i + 2, 1, k);
+      });
+      quarter(wo, a1, 1 - first, 1, [&](int k) {
+        if (WHICH == 2) return;
+        if (k == 0) arrive(WHICH == 1 ? left : kQBlock);
+        else if (k <= 4) read(a0, frag_a, k - 1);
+        if (k >= 5) issue(i + 3, 0, k - 5);
+      });
+      quarter(wf, a1, first, 1, [&](int k) {
+        if (WHICH == 2) return;
+        if (k < 4) read(wo, frag_w, k);
+        if (k == 4) advance(from);
+        if (k >= 3) issue(i + 3, 0, k);
+      });
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    if (none) mask(lds0, 0);
-    else issue(lds0, 0);
-    codes(0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    issue(lds1, 1);
-    read(a0, lds0, frag_a);
-    read(w0, lds0, frag_w);
+    if (none) {
+      mask(0, 0);
+      mask(kSlot, 0);
+      to = 2 * kSlot;
+    } else {
+      issue_all(0, 0);
+      issue_all(0, 1);
+    }
+    issue_all(1, 0);
+    issue_all(1, 1);
+#pragma unroll
+    for (int l = 0; l < 5; ++l) code(0, l);
+    arrive(kQBlock);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      read(a0, frag_a, c);
+      read(w0, frag_w, c);
+    }
+    issue_all(2, 0);
+    advance(from);
     int i = 0;
     for (; i + 2 < total; i += 2) {
-      step(lds0, lds1, i, 0, w0, w1, No{}, No{});
-      step(lds1, lds0, i + 1, 1, w1, w0, No{}, No{});
+      step(i, 0, w0, w1, std::integral_constant<int, 0>{});
+      step(i + 1, 1, w1, w0, std::integral_constant<int, 0>{});
     }
-    step(lds0, lds1, i, 0, w0, w1, Yes{}, No{});
-    step(lds1, lds0, i + 1, 1, w1, w0, No{}, Yes{});
+    step(i, 0, w0, w1, std::integral_constant<int, 1>{});
+    step(i + 1, 1, w1, w0, std::integral_constant<int, 2>{});
+    __builtin_amdgcn_s_waitcnt(0);  // what was fetched past the last block
   }
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
 #pragma unroll
@@ -618,7 +684,7 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = acc[j][t][8 * h + i];
-        store_run<8>(v, y + m * p.ldy, wn * 128 + j * 32 + 16 * g + 8 * h, count_n, p.act);
+        store_run<8>(v, y + m * p.ldy, wn * 128 + j * 32 + 16 * h + 8 * g, count_n, p.act);
       }
   }
 }
