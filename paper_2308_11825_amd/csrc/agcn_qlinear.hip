@@ -114,41 +114,62 @@ struct Rows {
   int32_t count, group;
 };
 
-// Tile `slot` of the rows cut at the groups' offsets. The rows before the first
+// The rows cut at the groups' offsets, in tiles of BM. The rows before the first
 // offset and after the last are parts of their own without a group, so that the
 // parts cover all rows. Offsets are clamped to [0, n] and a part that would be
 // negative is empty, so no offsets reach past the matrices. Every lane of a wave
-// calls it, with 64 parts looked at per step.
+// makes the calls, with 64 parts looked at per step.
 template <int BM>
-__device__ __forceinline__ Rows find_rows(const LinearArgs& p, int32_t slot) {
-  const int lane = threadIdx.x % 64, n = (int32_t)p.n;
-  const int parts = p.groups + 2;
-  for (int base = 0; base < parts; base += 64) {
-    const int i = base + lane;
-    int lo = 0, hi = 0;
+struct GroupTiles {
+  const int32_t* offsets;
+  int n, parts;
+  __device__ __forceinline__ GroupTiles(const LinearArgs& p)
+      : offsets(p.offsets), n((int)p.n), parts(p.groups + 2) {}
+  // The lane's part of a step: rows [*lo, *hi), and its tiles.
+  __device__ __forceinline__ int part(int base, int* lo, int* hi) const {
+    const int i = base + (int)(threadIdx.x % 64);
+    *lo = *hi = 0;
     if (i < parts) {
-      lo = i == 0 ? 0 : min(max(p.offsets[i - 1], 0), n);
-      hi = i == parts - 1 ? n : min(max(p.offsets[i], 0), n);
+      *lo = i == 0 ? 0 : min(max(offsets[i - 1], 0), n);
+      *hi = i == parts - 1 ? n : min(max(offsets[i], 0), n);
     }
-    const int tiles = hi > lo ? (int)(((int64_t)(hi - lo) + BM - 1) / BM) : 0;
-    int end = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int up = __shfl_up(end, d);
-      if (lane >= d) end += up;
-    }
-    const uint64_t hit = __ballot(slot < end);
-    if (hit != 0) {
-      const int at = __ffsll((unsigned long long)hit) - 1;
-      const int from = __shfl(lo, at), to = __shfl(hi, at);
-      const int tile = slot - (__shfl(end, at) - __shfl(tiles, at));
-      const int row = from + tile * BM, part = base + at;
-      return {row, min(BM, to - row), part == 0 || part == parts - 1 ? -1 : part - 1};
-    }
-    slot -= __shfl(end, 63);
+    return *hi > *lo ? (int)(((int64_t)(*hi - *lo) + BM - 1) / BM) : 0;
   }
-  return {0, 0, -1};
-}
+  __device__ __forceinline__ int total() const {
+    int sum = 0;
+    for (int base = 0; base < parts; base += 64) {
+      int lo, hi;
+      sum += part(base, &lo, &hi);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    return __builtin_amdgcn_readfirstlane(sum);
+  }
+  __device__ __forceinline__ Rows find(int tile) const {
+    const int lane = threadIdx.x % 64;
+    for (int base = 0; base < parts; base += 64) {
+      int lo, hi;
+      const int tiles = part(base, &lo, &hi);
+      int end = tiles;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int up = __shfl_up(end, d);
+        if (lane >= d) end += up;
+      }
+      const uint64_t hit = __ballot(tile < end);
+      if (hit != 0) {
+        const int at = __ffsll((unsigned long long)hit) - 1;
+        const int first = __shfl(end, at) - __shfl(tiles, at), i = base + at;
+        const int row = __shfl(lo, at) + (tile - first) * BM;
+        return {__builtin_amdgcn_readfirstlane(row),
+                __builtin_amdgcn_readfirstlane(min(BM, __shfl(hi, at) - row)),
+                __builtin_amdgcn_readfirstlane(i == 0 || i == parts - 1 ? -1 : i - 1)};
+      }
+      tile -= __shfl(end, 63);
+    }
+    return {0, 0, -1};
+  }
+};
 
 // Tiles that any offsets cut n rows into, at most.
 int64_t most_slots(int64_t n, int32_t groups, int64_t bm) {
@@ -165,7 +186,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
   const int n0 = blockIdx.x * 16;
   Rows rows;
   if constexpr (GROUPED) {
-    rows = find_rows<BM>(p, blockIdx.y);
+    rows = GroupTiles<BM>(p).find((int)blockIdx.y);
   } else {
     rows.row = (int64_t)blockIdx.y * BM;
     rows.count = (int32_t)min((int64_t)BM, p.n - rows.row);
@@ -355,44 +376,56 @@ struct RowScales {
 };
 
 // The rows and the column tile of this workgroup: bands of group_m row tiles, in each
-// the row tiles of one column tile after another.
+// the row tiles of one column tile after another. The grid of a grouped product
+// has room for any offsets; the tiles there are go to the first workgroups, so that all
+// XCDs have as many.
 template <int BM, bool GROUPED>
 __device__ __forceinline__ Rows tile_rows(const LinearArgs& p, uint32_t tiles_n, uint32_t group_m,
                                           uint32_t* tn) {
-  const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x), tiles_m = gridDim.x / tiles_n;
+  uint32_t tiles_m = gridDim.x / tiles_n;
+  if constexpr (GROUPED) {
+    tiles_m = (uint32_t)GroupTiles<BM>(p).total();
+    if (blockIdx.x >= tiles_m * tiles_n) return {0, 0, -1};
+  }
+  const uint32_t tile = xcd_tile(blockIdx.x, tiles_m * tiles_n);
   const uint32_t band = tile / (group_m * tiles_n), in = tile % (group_m * tiles_n);
   const uint32_t high = min(group_m, tiles_m - band * group_m);
-  const uint32_t tm = band * group_m + in % high;
-  *tn = in / high;
-  Rows rows;
-  if constexpr (GROUPED) {
-    rows = find_rows<BM>(p, (int)tm);
-    rows.row = __builtin_amdgcn_readfirstlane((int)rows.row);
-    rows.count = __builtin_amdgcn_readfirstlane(rows.count);
-    rows.group = __builtin_amdgcn_readfirstlane(rows.group);
-  } else {
-    rows.row = (int64_t)tm * BM;
-    rows.count = (int32_t)min((int64_t)BM, p.n - rows.row);
-    rows.group = 0;
-  }
-  return rows;
+  // (Divisions are vector code; the buffers built on their results must be scalar.)
+  const uint32_t tm = __builtin_amdgcn_readfirstlane(band * group_m + in % high);
+  *tn = __builtin_amdgcn_readfirstlane(in / high);
+  if constexpr (GROUPED) return GroupTiles<BM>(p).find((int)tm);
+  const int64_t row = (int64_t)tm * BM;
+  return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
 }
 
-// Writes RUN neighbouring outputs of a row from column n on, of `count` columns.
-template <int RUN, class TY>
-__device__ __forceinline__ void store_run(const float (&v)[RUN], TY* to, int n, int count, int32_t act) {
+// Writes RUN neighbouring outputs of a row from column n on, of `count` columns. ALL:
+// the caller knows that they are all there.
+template <bool ALL, int RUN, class TY>
+__device__ __forceinline__ void store_run(const float (&v)[RUN], TY* to, int n, int count) {
   struct alignas(sizeof(TY)) Run {
     TY e[RUN];
   } o;
 #pragma unroll
-  for (int i = 0; i < RUN; ++i) o.e[i] = (TY)q_act(v[i], act);
-  if (n + RUN <= count) {
+  for (int i = 0; i < RUN; ++i) o.e[i] = (TY)v[i];
+  if (ALL || n + RUN <= count) {
     store_any(to + n, o);
   } else {
 #pragma unroll
     for (int i = 0; i < RUN; ++i)
       if (n + i < count) to[n + i] = o.e[i];
   }
+}
+
+// Calls write(all, relu) with both as compile-time constants: whole tiles without
+// activation, most of them, then write nothing but their values.
+template <class F>
+__device__ __forceinline__ void write_tile(bool whole, int32_t act, F write) {
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (whole && act == 0) write(Yes{}, No{});
+  else if (whole) write(Yes{}, Yes{});
+  else if (act == 0) write(No{}, No{});
+  else write(No{}, Yes{});
 }
 
 // BM x BN outputs per workgroup of WM x WN waves, TM x TN a wave, one block of 128 k
@@ -496,19 +529,22 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
   }
 
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
-  constexpr int kRun = PERM ? 8 : 4;  // neighbouring outputs of a lane
+  write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
+    constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
+    constexpr int kRun = PERM ? 8 : 4;  // neighbouring outputs of a lane
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = wm * TM + t * 16 + r;
-    if (m >= rows.count) continue;
+    for (int t = 0; t < MT; ++t) {
+      const int m = wm * TM + t * 16 + r;
+      if (!ALL && m >= rows.count) continue;
 #pragma unroll
-    for (int j = 0; j < NT; j += kRun / 4) {
-      float v[kRun];
+      for (int j = 0; j < NT; j += kRun / 4) {
+        float v[kRun];
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) v[i] = acc[j + i / 4][t][i % 4];
-      store_run(v, y + m * p.ldy, wn * TN + (PERM ? j / 2 * 32 + 8 * g : j * 16 + 4 * g), count_n, p.act);
+        for (int i = 0; i < kRun; ++i) v[i] = q_act(acc[j + i / 4][t][i % 4], RELU);
+        store_run<ALL>(v, y + m * p.ldy, wn * TN + (PERM ? j / 2 * 32 + 8 * g : j * 16 + 4 * g), count_n);
+      }
     }
-  }
+  });
 }
 
 // 256 x 256 outputs per workgroup of 4 waves, 128 x 128 a wave: the accumulators fill
@@ -672,21 +708,45 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
     step(i + 1, 1, w1, w0, std::integral_constant<int, 2>{});
     __builtin_amdgcn_s_waitcnt(0);  // what was fetched past the last block
   }
+  // 32 rows at a time through the wave's own part of LDS, so that 16 lanes write 256
+  // neighbouring bytes of Y (a lane's own 16 bytes of 32 rows made 3 TB/s of the
+  // whole chip's writes). Rows are 16 bytes apart from a multiple of the banks.
+  __syncthreads();
+  constexpr int kRow = 128 * sizeof(TY) + 16;
+  uint8_t* own = lds + wave * 32 * kRow;
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
+  write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
+    constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
+    struct alignas(16) Run {
+      TY e[8];
+    };
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int m = wm * 128 + t * 32 + r;
-    if (m >= rows.count) continue;
+    for (int t = 0; t < 4; ++t) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float v[8];
+        for (int h = 0; h < 2; ++h) {
+          Run v;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[j][t][8 * h + i];
-        store_run<8>(v, y + m * p.ldy, wn * 128 + j * 32 + 16 * h + 8 * g, count_n, p.act);
+          for (int i = 0; i < 8; ++i) v.e[i] = (TY)q_act(acc[j][t][8 * h + i], RELU);
+          *reinterpret_cast<Run*>(own + r * kRow + (j * 32 + 16 * h + 8 * g) * sizeof(TY)) = v;
+        }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = i * 4 + lane / 16, m = wm * 128 + t * 32 + row, n = wn * 128 + lane % 16 * 8;
+        const Run v = *reinterpret_cast<const Run*>(own + row * kRow + lane % 16 * 16);
+        if (!ALL && m >= rows.count) continue;
+        TY* to = y + m * p.ldy + n;
+        if (ALL || n + 8 <= count_n) {
+          store_any(to, v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (n + k < count_n) to[k] = v.e[k];
+        }
       }
-  }
+    }
+  });
 }
 
 // Grid of a launch over BM x BN tiles; rows of a band: square patches of about 32
