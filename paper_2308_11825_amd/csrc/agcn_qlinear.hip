@@ -50,17 +50,6 @@ struct LinearArgs {
   int32_t act;
 };
 
-// The product of two scales, 2^(code + code - 254), as two factors: it may be out
-// of float's range where the scaled sum is not. A code of 255 is NaN.
-struct TwoFactors {
-  float a, b;
-};
-__device__ __forceinline__ TwoFactors scale_product(uint32_t sw, uint32_t sa) {
-  const int e = (int)(sw + sa) - 254, half = e >> 1;  // -254 to 254
-  const float a = __builtin_amdgcn_ldexpf(1.0f, half), b = __builtin_amdgcn_ldexpf(1.0f, e - half);
-  return {sw == 255 || sa == 255 ? __builtin_nanf("") : a, b};
-}
-
 // `valid` of 16 bytes, zeros in the others' place.
 __device__ __forceinline__ v4i load16(const uint8_t* p, int valid) {
   if (valid >= 16) return load_any<v4i>(p);
@@ -75,13 +64,17 @@ __device__ __forceinline__ v8i join(v4i a, v4i b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Eight of a lane's 32 values (words 2 j and 2 j + 1) as bf16, exactly.
-__device__ __forceinline__ v8b to_bf16(v8i v, int j) {
+// Eight of a lane's 32 values (words 2 j and 2 j + 1) times their scale as bf16, which
+// holds them exactly down to 2^-133 (its last subnormal; only values below 2^-129 with
+// one of the three least scales have bits there). The conversion takes a scale as a
+// float's exponent, code 0 as 2^-127 and 255 as NaN.
+__device__ __forceinline__ v8b to_bf16(v8i v, int j, uint32_t code) {
+  const float scale = __builtin_bit_cast(float, code << 23);
   v8b r;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * j + h], 1.0f, false);
-    const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * j + h], 1.0f, true);
+    const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * j + h], scale, false);
+    const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * j + h], scale, true);
     r[4 * h] = a[0];
     r[4 * h + 1] = a[1];
     r[4 * h + 2] = b[0];
@@ -90,20 +83,43 @@ __device__ __forceinline__ v8b to_bf16(v8i v, int j) {
   return r;
 }
 
-// acc += s_w s_a (w a) for one block of 128 k. A lane holds 32 k of row
-// lane % 16 of both; which 32 does not matter as long as both agree.
-template <bool EXACT>
-__device__ __forceinline__ void block_product(v4f& acc, v8i w, v8i a, uint32_t sw, uint32_t sa) {
+// acc[j][t] += scaled w[j] a[t] for one block of 128 k. `w` and `a` give the 32 values
+// that a lane holds of row lane % 16; which 32 does not matter as long as both
+// agree. EXACT: on the bf16 matrix cores.
+template <bool EXACT, int NT, int MT, class GetW, class GetA>
+__device__ __forceinline__ void block_products(v4f (&acc)[NT][MT], GetW w, GetA a, uint32_t sw,
+                                               const uint32_t (&sa)[MT]) {
   if constexpr (EXACT) {
-    v4f part = {0.0f, 0.0f, 0.0f, 0.0f};
+    v8b ab[MT][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(w, j), to_bf16(a, j), part, 0, 0, 0);
-    const TwoFactors f = scale_product(sw, sa);
+    for (int t = 0; t < MT; ++t) {
+      const v8i av = a(t);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = fmaf(part[i] * f.a, f.b, acc[i]);
+      for (int i = 0; i < 4; ++i) ab[t][i] = to_bf16(av, i, sa[t]);
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const v8i wv = w(j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const v8b wb = to_bf16(wv, i, sw);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, ab[t][i], acc[j][t], 0, 0, 0);
+      }
+    }
   } else {
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, acc, 0, 0, 0, (int)sw, 0, (int)sa);
+    v8i av[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) av[t] = a(t);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const v8i wv = w(j);
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+        acc[j][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av[t], acc[j][t], 0, 0, 0,
+                                                                     (int)sw, 0, (int)sa[t]);
+    }
   }
 }
 
@@ -145,11 +161,13 @@ struct GroupTiles {
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     return __builtin_amdgcn_readfirstlane(sum);
   }
+  // Tile `tile` of all parts' tiles but the first SKIP of each.
+  template <int SKIP>
   __device__ __forceinline__ Rows find(int tile) const {
     const int lane = threadIdx.x % 64;
     for (int base = 0; base < parts; base += 64) {
       int lo, hi;
-      const int tiles = part(base, &lo, &hi);
+      const int tiles = max(part(base, &lo, &hi) - SKIP, 0);
       int end = tiles;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
@@ -160,7 +178,7 @@ struct GroupTiles {
       if (hit != 0) {
         const int at = __ffsll((unsigned long long)hit) - 1;
         const int first = __shfl(end, at) - __shfl(tiles, at), i = base + at;
-        const int row = __shfl(lo, at) + (tile - first) * BM;
+        const int row = __shfl(lo, at) + (SKIP + tile - first) * BM;
         return {__builtin_amdgcn_readfirstlane(row),
                 __builtin_amdgcn_readfirstlane(min(BM, __shfl(hi, at) - row)),
                 __builtin_amdgcn_readfirstlane(i == 0 || i == parts - 1 ? -1 : i - 1)};
@@ -171,34 +189,51 @@ struct GroupTiles {
   }
 };
 
+// The rows of workgroup y where groups have few: the first BM of part y, found without
+// a search; tiles past a part's first go to the workgroups after the parts'.
+template <int BM, bool GROUPED>
+__device__ __forceinline__ Rows few_rows(const LinearArgs& p) {
+  if constexpr (!GROUPED) {
+    const int64_t row = (int64_t)blockIdx.y * BM;
+    return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
+  } else {
+    const int n = (int)p.n, i = blockIdx.y, last = p.groups + 1;
+    if (i > last) return GroupTiles<BM>(p).template find<1>(i - last - 1);
+    const int lo = i == 0 ? 0 : min(max(p.offsets[i - 1], 0), n);
+    const int hi = i == last ? n : min(max(p.offsets[i], 0), n);
+    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(min(BM, hi - lo)),
+            i == 0 || i == last ? -1 : i - 1};
+  }
+}
+int64_t few_rows_grid(int64_t n, int32_t groups, int64_t bm, bool grouped) {
+  return grouped ? groups + 2 + n / bm : ceil_div64(n, bm);
+}
+
 // Tiles that any offsets cut n rows into, at most.
 int64_t most_slots(int64_t n, int32_t groups, int64_t bm) {
   return std::min<int64_t>(n, n / bm + groups + 2);
 }
 
-// One workgroup: 16 outputs by MT * 16 rows, its waves taking the blocks of k in
-// turn, each straight from memory; their sums are added in the waves' order.
-template <int MT, int NW, bool EXACT, class TY, bool GROUPED>
+// --- few rows, any alignment: straight from memory ---------------------------------------
+
+// One workgroup: 16 outputs by MT * 16 rows. Its NW waves take the blocks of k in turn, U
+// at a time so that their loads are on their way together; their sums are added in
+// the waves' order.
+template <int MT, int NW, int U, bool EXACT, class TY, bool GROUPED>
 __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
-  __shared__ float part[NW][MT * 16][16];
   constexpr int BM = MT * 16;
+  __shared__ float part[NW][BM][20];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
   const int n0 = blockIdx.x * 16;
-  Rows rows;
-  if constexpr (GROUPED) {
-    rows = GroupTiles<BM>(p).find((int)blockIdx.y);
-  } else {
-    rows.row = (int64_t)blockIdx.y * BM;
-    rows.count = (int32_t)min((int64_t)BM, p.n - rows.row);
-    rows.group = 0;
-  }
+  const Rows rows = few_rows<BM, GROUPED>(p);
   if (rows.count <= 0) return;
-  v4f acc[MT];
+  v4f acc[1][MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < MT; ++t) acc[0][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   if (rows.group >= 0) {
     // Rows past the last are read as the last; their results are not written.
-    const uint8_t* w = p.W + rows.group * p.group_w + (int64_t)min(n0 + r, p.fout - 1) * p.ldw + g * 32;
+    const uint8_t* w =
+        p.W + rows.group * p.group_w + (int64_t)min(n0 + r, p.fout - 1) * p.ldw + g * 32;
     const uint8_t* sw = p.SW + rows.group * p.group_sw + (int64_t)(n0 / kQBlock) * p.ldsw;
     const uint8_t *a[MT], *sa[MT];
 #pragma unroll
@@ -207,20 +242,45 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
       a[t] = p.A + m * p.lda + g * 32;
       sa[t] = p.SA + m * p.ldsa;
     }
-    const int whole = p.fin / kQBlock, blocks = (p.fin + kQBlock - 1) / kQBlock;
-    for (int b = wave; b < blocks; b += NW) {
-      const int valid = b < whole ? 32 : p.fin - b * kQBlock - g * 32;
+    struct Block {
+      v8i w, a[MT];
+      uint32_t sw, sa[MT];
+    };
+    auto load = [&](Block& v, int b, int valid) {
       const int64_t k = (int64_t)b * kQBlock;
-      const v8i wv = join(load16(w + k, valid), load16(w + k + 16, valid - 16));
+      v.w = join(load16(w + k, valid), load16(w + k + 16, valid - 16));
+      v.sw = sw[b];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        const v8i av = join(load16(a[t] + k, valid), load16(a[t] + k + 16, valid - 16));
-        block_product<EXACT>(acc[t], wv, av, sw[b], sa[t][b]);
+        v.a[t] = join(load16(a[t] + k, valid), load16(a[t] + k + 16, valid - 16));
+        v.sa[t] = sa[t][b];
       }
+    };
+    auto multiply = [&](const Block& v) {
+      block_products<EXACT>(acc, [&](int) { return v.w; }, [&](int t) { return v.a[t]; }, v.sw, v.sa);
+    };
+    const int whole = p.fin / kQBlock, left = p.fin % kQBlock;
+    int b = wave;
+    for (; b + (U - 1) * NW < whole; b += U * NW) {
+      Block v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load(v[u], b + u * NW, 32);
+#pragma unroll
+      for (int u = 0; u < U; ++u) multiply(v[u]);
+    }
+    for (; b < whole; b += NW) {
+      Block v;
+      load(v, b, 32);
+      multiply(v);
+    }
+    if (left != 0 && b == whole) {
+      Block v;
+      load(v, b, left - g * 32);
+      multiply(v);
     }
   }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) store_any(&part[wave][t * 16 + r][g * 4], acc[t]);
+  for (int t = 0; t < MT; ++t) *reinterpret_cast<v4f*>(&part[wave][t * 16 + r][g * 4]) = acc[0][t];
   __syncthreads();
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
   for (int i = threadIdx.x; i < rows.count * 16; i += 64 * NW) {
@@ -230,15 +290,6 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
     for (int k = 1; k < NW; ++k) v += part[k][m][n];
     if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(v, p.act);
   }
-}
-
-template <int MT, int NW, bool EXACT, class TY, bool GROUPED>
-int launch_thin(const LinearArgs& p, hipStream_t st) {
-  const int64_t y = GROUPED ? most_slots(p.n, p.groups, MT * 16) : ceil_div64(p.n, MT * 16);
-  const dim3 grid((unsigned)ceil_div64(p.fout, 16), (unsigned)y);
-  k_qlinear_thin<MT, NW, EXACT, TY, GROUPED><<<grid, 64 * NW, 0, st>>>(p);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? AGCN_OK : hip_fail(e, "k_qlinear_thin launch");
 }
 
 // --- tiles through LDS -------------------------------------------------------------
@@ -393,7 +444,7 @@ __device__ __forceinline__ Rows tile_rows(const LinearArgs& p, uint32_t tiles_n,
   // (Divisions are vector code; the buffers built on their results must be scalar.)
   const uint32_t tm = __builtin_amdgcn_readfirstlane(band * group_m + in % high);
   *tn = __builtin_amdgcn_readfirstlane(in / high);
-  if constexpr (GROUPED) return GroupTiles<BM>(p).find((int)tm);
+  if constexpr (GROUPED) return GroupTiles<BM>(p).template find<0>((int)tm);
   const int64_t row = (int64_t)tm * BM;
   return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
 }
@@ -498,22 +549,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
       __syncthreads();
     };
     auto multiply = [&](const uint8_t* lds) {
-      v8i a[MT];
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const uint8_t* at = lds + frag_a + t * 16 * kQBlock;
-        a[t] = join(*reinterpret_cast<const v4i*>(at),
-                    *reinterpret_cast<const v4i*>(lds + ((frag_a + t * 16 * kQBlock) ^ 64)));
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int row = PERM ? j / 2 * 32 + j % 2 * 4 : j * 16;
-        const int at = frag_w + row * kQBlock;
-        const v8i w = join(*reinterpret_cast<const v4i*>(lds + at),
-                           *reinterpret_cast<const v4i*>(lds + (at ^ 64)));
-#pragma unroll
-        for (int t = 0; t < MT; ++t) block_product<EXACT>(acc[j][t], w, a[t], code_w, code_a[t]);
-      }
+      auto read = [&](int at) {
+        return join(*reinterpret_cast<const v4i*>(lds + at), *reinterpret_cast<const v4i*>(lds + (at ^ 64)));
+      };
+      block_products<EXACT>(
+          acc, [&](int j) { return read(frag_w + (PERM ? j / 2 * 32 + j % 2 * 4 : j * 16) * kQBlock); },
+          [&](int t) { return read(frag_a + t * 16 * kQBlock); }, code_w, code_a);
     };
     fetch(lds0, 0);
     arrive(lds0, 0);
@@ -545,6 +586,128 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
       }
     }
   });
+}
+
+// --- few rows: every wave streams blocks of k of its own ------------------------------
+
+// ROWS rows of a block of 128 k, staged by one wave for itself.
+template <int ROWS>
+struct WaveStage {
+  const uint8_t* base;
+  uint32_t bytes, first;
+  int32_t ld, piece;
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t stride, int rows, int fin, int lane) {
+    base = p;
+    ld = (int32_t)stride;
+    bytes = (uint32_t)(rows - 1) * (uint32_t)ld + (((uint32_t)fin + 3) & ~3u);
+    first = (uint32_t)(lane / 8 * ld);
+  }
+  // Eight rows further the swizzle is another.
+  static __device__ __forceinline__ int piece_of(int i, int lane) {
+    return ((lane % 8) ^ swizzle_key<0>(i * 8 + lane / 8)) * 16;
+  }
+  __device__ __forceinline__ void issue(uint8_t* lds, uint32_t k, int lane) const {
+    const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          res, (__attribute__((address_space(3))) void*)(lds + i * 1024), 16,
+          first + ((uint32_t)(i * 8 * ld) + k) + piece_of(i, lane), 0, 0, 0);
+  }
+  __device__ __forceinline__ void mask(uint8_t* lds, int left, int lane) const {
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i)
+      *reinterpret_cast<v4i*>(lds + i * 1024 + lane * 16) &= bytes_kept(left - piece_of(i, lane));
+  }
+};
+
+// One workgroup: NT * 16 outputs by MT * 16 rows. Its NW waves take the blocks of k in
+// turn, each through S slots of LDS of its own that are filled S - 1 blocks ahead, so no
+// wave waits for another before the end, where their sums are added in the waves'
+// order. Bound by the loads on their way: through LDS 8 lanes read 128 neighbouring
+// bytes, where a fragment read straight into registers takes 16 bytes of 16 rows per 16
+// lanes and its time from the address unit (64 x 4096 -> 4096 17.5 us, and 8.5 here).
+template <int MT, int NT, int NW, int S, bool EXACT, class TY, bool GROUPED>
+__global__ __launch_bounds__(64 * NW) void k_qlinear_stream(LinearArgs p) {
+  constexpr int BM = MT * 16, BN = NT * 16, kStage = (BM + BN) * kQBlock;
+  constexpr int kLoads = (BM + BN) / 8 + MT + 1;  // of a block: into LDS, and scales
+  constexpr int kSums = NW * BM * (BN + 4) * 4;
+  static_assert(kQBlock % BN == 0 && kLoads * (S - 1) < 64, "one scale of W, and vmcnt's range");
+  __shared__ __align__(1024) uint8_t lds[NW * S * kStage > kSums ? NW * S * kStage : kSums];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane % 16, g = lane / 16, n0 = blockIdx.x * BN;
+  const Rows rows = few_rows<BM, GROUPED>(p);
+  if (rows.count <= 0) return;
+  const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
+  const int mine = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
+  v4f acc[NT][MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  if (mine > 0) {
+    uint8_t* own = lds + wave * S * kStage;
+    WaveStage<BN> sw;
+    sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, min(BN, p.fout - n0), p.fin, lane);
+    const uint8_t* scale_w = p.SW + rows.group * p.group_sw + (int64_t)(n0 / kQBlock) * p.ldsw;
+    WaveStage<BM> sa;
+    sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, lane);
+    RowScales<16> scale_a;
+    scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, r);
+    const int frag = r * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
+    uint32_t code_a[S][MT], code_w[S];
+    // The wave's i-th block, into slot u = i % S; past the last one zeros.
+    auto fetch = [&](int i, int u) {
+      const int b = wave + i * NW;
+      const uint32_t k = i < mine ? (uint32_t)(b * kQBlock) : 0x80000000u;
+      sw.issue(own + u * kStage, k, lane);
+      sa.issue(own + u * kStage + BN * kQBlock, k, lane);
+      const int c = min(b, blocks - 1);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) code_a[u][t] = scale_a.load(t, c);
+      code_w[u] = scale_w[c];
+    };
+#pragma unroll
+    for (int u = 0; u < S - 1; ++u) fetch(u, u);
+    for (int i0 = 0; i0 < mine; i0 += S) {
+#pragma unroll
+      for (int u = 0; u < S; ++u) {
+        fetch(i0 + u + S - 1, (u + S - 1) % S);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads*(S - 1)) : "memory");
+        uint8_t* slot = own + u * kStage;
+        const int left = p.fin - (wave + (i0 + u) * NW) * kQBlock;
+        if (left < kQBlock) {
+          sw.mask(slot, left, lane);
+          sa.mask(slot + BN * kQBlock, left, lane);
+        }
+        auto read = [&](int at) {
+          return join(*reinterpret_cast<const v4i*>(slot + at), *reinterpret_cast<const v4i*>(slot + (at ^ 64)));
+        };
+        block_products<EXACT>(
+            acc, [&](int j) { return read(frag + j * 16 * kQBlock); },
+            [&](int t) { return read(frag + (BN + t * 16) * kQBlock); }, code_w[u], code_a[u]);
+        // The slot is filled again by the next fetch: its reads are over.
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // what was fetched past the last block
+  __syncthreads();
+  auto part = reinterpret_cast<float(*)[BM][BN + 4]>(lds);
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+      *reinterpret_cast<v4f*>(&part[wave][t * 16 + r][j * 16 + g * 4]) = acc[j][t];
+  __syncthreads();
+  TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
+  for (int i = threadIdx.x; i < rows.count * BN; i += 64 * NW) {
+    const int m = i / BN, n = i % BN;
+    float v = part[0][m][n];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) v += part[k][m][n];
+    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(v, p.act);
+  }
 }
 
 // 256 x 256 outputs per workgroup of 4 waves, 128 x 128 a wave: the accumulators fill
@@ -594,7 +757,7 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
     const int frag_a = (wm * 64 + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
     const int frag_w = kPart + (wn * 64 + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
 
-    uint32_t code_a[4], next_a[4], code_w, next_w;
+    uint32_t code_a[4], next_a[2][4], code_w, next_w[2];
     int to = 0, from = 0;  // slots to fill and to read next
     auto advance = [](int& slot) { slot = slot == (kSlots - 1) * kSlot ? 0 : slot + kSlot; };
     // Half h of block i: rows 64 h to 64 h + 63 of every 128 of A, and of W the other
@@ -610,10 +773,12 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
 #pragma unroll
       for (int l = 0; l < 8; ++l) issue(i, h, l);
     };
-    auto code = [&](int i, int l) {
-      const int b = max(i - none, 0);
-      if (l < 4) next_a[l] = scale_a.load(l, b);
-      else next_w = scale_w[b];
+    // Two blocks ahead: loads arrive in their order, and a block's scales are asked for
+    // after the values of the first half of the block after the next.
+    auto code = [&](int i, int u, int l) {
+      const int b = min(max(i - none, 0), blocks - 1);
+      if (l < 4) next_a[u][l] = scale_a.load(l, b);
+      else next_w[u] = scale_w[b];
     };
     auto mask = [&](int slot, int left) {
       sa.mask(lds + slot, left, wave, lane);
@@ -651,14 +816,14 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
       constexpr int WHICH = decltype(which)::value;
       const int left = WHICH == 0 ? kQBlock : p.fin - (blocks - 1) * kQBlock;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) code_a[t] = next_a[t];
-      code_w = next_w;
+      for (int t = 0; t < 4; ++t) code_a[t] = next_a[first][t];
+      code_w = next_w[first];
       // At most one load after a product: the four waves' loads are taken in turn.
       quarter(wf, a0, first, 0, [&](int k) {
         if (k == 0) arrive(WHICH == 2 ? left : kQBlock);
         else if (k <= 4) read(wo, frag_w, k - 1);
         if (WHICH == 2) return;
-        if (k >= 1 && k < 6) code(i + 1, k - 1);
+        if (k >= 1 && k < 6) code(i + 2, first, k - 1);
         if (k >= 6) issue(i + 2, 1, k - 6);
       });
       quarter(wo, a0, 1 - first, 0, [&](int k) {
@@ -690,7 +855,7 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
     issue_all(1, 0);
     issue_all(1, 1);
 #pragma unroll
-    for (int l = 0; l < 5; ++l) code(0, l);
+    for (int l = 0; l < 10; ++l) code(l / 5, l / 5, l % 5);
     arrive(kQBlock);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -785,26 +950,92 @@ int launch_big(const LinearArgs& p, hipStream_t st) {
   return launched("k_qlinear_big launch");
 }
 
+template <int MT, int U, bool EXACT, class TY, bool GROUPED>
+int launch_thin(const LinearArgs& p, hipStream_t st) {
+  constexpr int NW = 8;
+  const dim3 grid((unsigned)ceil_div64(p.fout, 16), (unsigned)few_rows_grid(p.n, p.groups, MT * 16, GROUPED));
+  k_qlinear_thin<MT, NW, U, EXACT, TY, GROUPED><<<grid, 64 * NW, 0, st>>>(p);
+  return launched("k_qlinear_thin launch");
+}
+
+template <int MT, int NT, int NW, int S, bool EXACT, class TY, bool GROUPED>
+int launch_stream(const LinearArgs& p, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div64(p.fout, NT * 16),
+                  (unsigned)few_rows_grid(p.n, p.groups, MT * 16, GROUPED));
+  k_qlinear_stream<MT, NT, NW, S, EXACT, TY, GROUPED><<<grid, 64 * NW, 0, st>>>(p);
+  return launched("k_qlinear_stream launch");
+}
+
+// Which kernel. Figures are us on one MI355X, bfloat16 outputs; the float32 ones, without
+// k_qlinear_big, cross at the same places.
 template <bool EXACT, class TY, bool GROUPED>
 int linear_typed(const LinearArgs& p, hipStream_t st) {
+  constexpr int64_t kUnits = 256;  // compute units
+  // Into LDS directly: rows that start on 16 bytes.
   const bool async = aligned16(p.A) && aligned16(p.W) && p.lda % 16 == 0 && p.ldw % 16 == 0 &&
-                     p.group_w % 16 == 0;
+                     (!GROUPED || p.group_w % 16 == 0);
   // Offsets inside a tile are 32-bit.
   const bool near = std::max({p.lda, p.ldw, p.ldsa}) <= (INT32_MAX - kMostWidth) / 256;
-  if (near && p.n > 64) {
-    if constexpr (!EXACT)
-      if (async && p.n >= 256) return launch_big<TY, GROUPED>(p, st);
-    if (async) return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, true>(p, st);
-    return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, false>(p, st);
+  const int64_t rows = GROUPED ? p.n / std::max(1, p.groups) : p.n;  // of a group, on average
+  const bool fits_y = few_rows_grid(p.n, p.groups, 16, GROUPED) <= 65535;  // a grid's y
+  // Row and column tiles together, half a row tile more per group.
+  auto tiles = [&](int64_t bm, int64_t bn) {
+    const int64_t m = GROUPED ? p.n / bm + (p.groups + 1) / 2 : ceil_div64(p.n, bm);
+    return m * ceil_div64(p.fout, bn);
+  };
+  if (!near || !async) {
+    if (fits_y && (!near || rows <= 64)) {
+      if (rows <= 16) return launch_thin<1, 4, EXACT, TY, GROUPED>(p, st);
+      return launch_thin<2, 2, EXACT, TY, GROUPED>(p, st);
+    }
+    if (!near) return fail(AGCN_ERR_UNSUPPORTED, "row strides over 8 million bytes and over 65535 row tiles");
+    if (tiles(64, 64) <= 4 * kUnits) return launch_tile<32, 32, 2, 2, EXACT, TY, GROUPED, false>(p, st);
+    return launch_tile<32, 64, 4, 1, EXACT, TY, GROUPED, false>(p, st);
   }
-  return launch_thin<4, 4, EXACT, TY, GROUPED>(p, st);
+  if constexpr (GROUPED) {
+    // Few rows a group: bound by the weights, which are read once per row tile. 512 x 4096
+    // -> 2048 over 64 groups 93 with 32 x 32 outputs, 99 with 64 x 64 and 148 in k_qlinear_tile;
+    // 2048 rows 151, 125 and 155; 4096 rows 236, 169 and 164 (k_qlinear_big).
+    if (fits_y && rows <= 12) return launch_stream<2, 2, 4, 2, EXACT, TY, true>(p, st);
+    if (fits_y && rows < 64) return launch_stream<4, 4, 4, 1, EXACT, TY, true>(p, st);
+  } else if (tiles(64, 64) <= kUnits) {
+    // Few outputs: the largest tile of which there are not more than compute units, each
+    // read by a workgroup that splits k over its waves. 16, 64, 128 and 256 x 4096 -> 4096:
+    // 6.6, 11.2, 19.8, 36 with 16 x 32 outputs; 7.2, 8.5, 13.2, 22 with 32 x 32; 8.6, 10.0, 10.9,
+    // 18 with 32 x 64; 10.7, 13.7, 13.9, 14.5 with 64 x 64; k_qlinear_tile 20 to 24.
+    if (tiles(16, 32) <= kUnits) return launch_stream<1, 2, 8, 2, EXACT, TY, false>(p, st);
+    if (tiles(32, 32) <= kUnits) return launch_stream<2, 2, 4, 2, EXACT, TY, false>(p, st);
+    if (tiles(32, 64) <= kUnits) return launch_stream<2, 4, 4, 2, EXACT, TY, false>(p, st);
+    return launch_stream<4, 4, 4, 2, EXACT, TY, false>(p, st);
+  } else if (tiles(64, 64) <= 2 * kUnits && p.fin >= 4096) {
+    // Two workgroups a compute unit and a long k: 512 x 4096 -> 4096 22.5, k_qlinear_tile 25;
+    // 1024 x 2048 -> 2048 13.5 and 12.9.
+    return launch_stream<4, 4, 4, 1, EXACT, TY, false>(p, st);
+  }
+  // The matrix cores bound it from half a tile per compute unit on: 2048 x 4096 -> 4096 47, 55 in
+  // tiles of 128; 1024 x 4096 -> 4096 42 and 34. Short k end before its loads are under way
+  // (65536 x 512 -> 512 31 and 32), and half-empty column tiles cost what full ones do (65536 x
+  // 1024 -> 128 30 and 18).
+  if constexpr (!EXACT)
+    if (rows >= 256 && p.fin >= 1024 && tiles(256, 256) >= kUnits / 2 &&
+        tiles(256, 256) * 16 <= tiles(128, 128) * 5)
+      return launch_big<TY, GROUPED>(p, st);
+  // Narrow outputs fill narrow tiles: 230,000 x 128 -> 41 13.7 with 64 columns, 22.5 with 128;
+  // 230,000 x 256 -> 16 13.6 with 32 columns, 16.8 with 64.
+  if (p.fout <= 32 && tiles(128, 32) >= kUnits) return launch_tile<32, 32, 4, 1, EXACT, TY, GROUPED, true>(p, st);
+  // Large tiles read less, small ones fill the chip: 16384 x 512 -> 512 (512 tiles of 128)
+  // 11.6, 13.0 with 128 x 64; 4096 x 1024 -> 1024 11.7 and 11.3; 1024 x 2048 -> 2048 17.1, 14.6 and 12.9 with
+  // 64 x 64.
+  if (p.fout > 64 && tiles(128, 128) >= 2 * kUnits) return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, true>(p, st);
+  if (tiles(128, 64) > kUnits) return launch_tile<32, 64, 4, 1, EXACT, TY, GROUPED, true>(p, st);
+  return launch_tile<32, 32, 2, 2, EXACT, TY, GROUPED, true>(p, st);
 }
 
 template <bool EXACT, class TY>
 int linear_pieces(const LinearArgs& p, hipStream_t st) {
   if (p.offsets != nullptr) return linear_typed<EXACT, TY, true>(p, st);
-  // A launch's row tiles: longer matrices go in pieces.
-  constexpr int64_t kMost = 65535 * 64;
+  // A launch's row tiles (at least of 16 rows): longer matrices go in pieces.
+  constexpr int64_t kMost = 65535 * 16;
   for (int64_t r = 0; r < p.n; r += kMost) {
     LinearArgs q = p;
     q.n = std::min(kMost, p.n - r);
