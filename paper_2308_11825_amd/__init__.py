@@ -515,35 +515,54 @@ def linear(X, W, out=None, stream=None):
 # one per 128 x 128 block of a weight. It stands for Q times its scales.
 
 _DTYPES = {}  # torch dtype -> AGCN_FLOAT, AGCN_BFLOAT, AGCN_HALF
+_torch = None
+_Q8 = _S8 = None  # the dtypes of values and of scales
 
 
-def _dtype_code(dtype):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: AGCN_FLOAT, torch.bfloat16: AGCN_BFLOAT,
-                        torch.float16: AGCN_HALF})
-    return _DTYPES.get(dtype)
-
-
-def _check_2d(name, t, device, shape=None, dtype=None, dims=2):
-    """Refuses what is not a matrix (or `dims` - 2 leading axes of them) on `device`
-    with unit column stride, of one of the three types or of `dtype`."""
+def _load_torch():
+    global _torch, _Q8, _S8
     import torch
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.device != device:
-        raise TypeError(f"{name} must be a CUDA tensor on the inputs' device")
-    if _dtype_code(t.dtype) is None if dtype is None else t.dtype != dtype:
-        raise TypeError(f"{name} must have dtype "
-                        f"{'float32, bfloat16 or float16' if dtype is None else dtype}")
-    if t.dim() != dims or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must have {dims} dimensions"
-                         + ("" if shape is None else f" and shape {shape}"))
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    _DTYPES.update({torch.float32: AGCN_FLOAT, torch.bfloat16: AGCN_BFLOAT,
+                    torch.float16: AGCN_HALF})
+    _Q8, _S8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    _torch = torch
+
+
+def _matrix(name, t, device, shape, dtype):
+    """The row stride of `t`, a matrix (or stacked ones) of this shape and type on `device`
+    with unit column stride; refuses anything else. (In one pass over what a right
+    tensor has: these checks are the larger part of a small call's time.)"""
+    if isinstance(t, _torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device:
+        stride = t.stride()
+        if stride[-1] == 1 and shape[-2] > 1:
+            return stride[-2]
+        if shape[-1] <= 1 or t.numel() == 0 or stride[-1] == 1:
+            # Any value >= a row is valid for 0 or 1 rows.
+            return stride[-2] if shape[-2] > 1 else max(shape[-1], stride[-2])
         raise ValueError(f"{name} must have unit column stride")
+    if not isinstance(t, _torch.Tensor) or t.device != device:
+        raise TypeError(f"{name} must be a tensor on {device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}")
+    raise ValueError(f"{name} must have shape {tuple(shape)}")
 
 
-def _ld(t):
-    """Row stride of the last two axes (any value >= a row is valid for 0 or 1 rows)."""
-    return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], t.stride(-2))
+def _first(name, t, dims):
+    """The shape and device of the tensor that sets a call's sizes and type."""
+    if _torch is None:
+        _load_torch()
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
+    return t.shape, t.device
+
+
+def _dtype_code(name, dtype):
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} must have dtype float32, bfloat16 or float16")
+    return code
 
 
 def _on_stream(device, stream, tensors):
@@ -557,43 +576,37 @@ def _on_stream(device, stream, tensors):
     return stream.cuda_stream
 
 
-def _allocate(device, stream, *shapes):
-    """Tensors of (shape, dtype), allocated on the stream that writes them."""
-    import torch
+def _new(like, stream, shape, dtype):
+    """A tensor on like's device, allocated on the stream that writes it."""
     if stream is None:
-        return [torch.empty(s, dtype=d, device=device) for s, d in shapes]
-    with torch.cuda.stream(stream):
-        return [torch.empty(s, dtype=d, device=device) for s, d in shapes]
+        return like.new_empty(shape, dtype=dtype)
+    with _torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _allocate_8bit(device, stream, lead, k, scale_rows, *more):
-    """Q (..., k) with rows that start on 16 bytes, and S."""
-    import torch
-    q, s, *rest = _allocate(device, stream, ((*lead, (k + 15) // 16 * 16), torch.float8_e4m3fn),
-                            ((*scale_rows, (k + 127) // 128), torch.float8_e8m0fnu), *more)
-    return (q[..., :k] if k % 16 else q), s, *rest
-
-
-def _check_8bit(names, Q, S, device, lead, k, scale_rows):
-    import torch
-    _check_2d(names[0], Q, device, (*lead, k), torch.float8_e4m3fn, len(lead) + 1)
-    _check_2d(names[1], S, device, (*scale_rows, (k + 127) // 128), torch.float8_e8m0fnu,
-              len(lead) + 1)
+def _new_rows(like, stream, lead, k):
+    """Values (..., k) in 8 bits with rows that start on 16 bytes, and their row stride."""
+    ld = (k + 15) // 16 * 16
+    q = _new(like, stream, (*lead, ld), _Q8)
+    return (q[..., :k] if k != ld else q), ld
 
 
 def quantize(X, out=None, stream=None):
     """The rows of X (n, f) in 8 bits: (Q, S). X: float32, bfloat16 or float16 CUDA
     tensor; out: such a pair to write to."""
-    _check_2d("X", X, getattr(X, "device", None))
-    n, f = X.shape
+    (n, f), device = _first("X", X, 2)
+    dtype = X.dtype
+    code, ldx, blocks = _dtype_code("X", dtype), _matrix("X", X, device, X.shape, dtype), (f + 127) // 128
     if out is None:
-        Q, S = _allocate_8bit(X.device, stream, (n,), f, (n,))
+        Q, ldq = _new_rows(X, stream, (n,), f)
+        S, lds = _new(X, stream, (n, blocks), _S8), blocks
     else:
         Q, S = out
-        _check_8bit(("out[0]", "out[1]"), Q, S, X.device, (n,), f, (n,))
-    st = _on_stream(X.device, stream, (X, Q, S))
-    _call(X.device, agcn_quantize_rows, n, f, _dtype_code(X.dtype), X.data_ptr(), _ld(X),
-          Q.data_ptr(), _ld(Q), S.data_ptr(), _ld(S), st)
+        ldq = _matrix("out[0]", Q, device, (n, f), _Q8)
+        lds = _matrix("out[1]", S, device, (n, blocks), _S8)
+    st = _on_stream(device, stream, (X, Q, S))
+    _call(device, agcn_quantize_rows, n, f, code, X.data_ptr(), ldx, Q.data_ptr(), ldq,
+          S.data_ptr(), lds, st)
     return Q, S
 
 
@@ -601,15 +614,17 @@ def quantize_weight(W, stream=None):
     """A weight (fin, fout), as ``linear`` takes it, or one per group (groups, fin,
     fout), in 8 bits for ``quantized_linear`` and ``grouped_linear``: (WQ, WS) with WQ
     (..., fout, fin), transposed, and WS (..., ceil(fout / 128), ceil(fin / 128))."""
-    dims = W.dim() if hasattr(W, "dim") and W.dim() == 3 else 2
-    _check_2d("W", W, getattr(W, "device", None), dims=dims)
-    *lead, fin, fout = W.shape
-    Q, S = _allocate_8bit(W.device, stream, (*lead, fout), fin, (*lead, (fout + 127) // 128))
-    st = _on_stream(W.device, stream, (W,))
+    shape, device = _first("W", W, 3 if getattr(W, "ndim", 2) == 3 else 2)
+    *lead, fin, fout = shape
+    dtype = W.dtype
+    code, ldw = _dtype_code("W", dtype), _matrix("W", W, device, shape, dtype)
+    nb, kb = (fout + 127) // 128, (fin + 127) // 128
+    Q, ldq = _new_rows(W, stream, (*lead, fout), fin)
+    S = _new(W, stream, (*lead, nb, kb), _S8)
+    st = _on_stream(device, stream, (W,))
     groups, strides = (lead[0], [t.stride(0) for t in (W, Q, S)]) if lead else (1, (0, 0, 0))
-    _call(W.device, agcn_quantize_weight, groups, fin, fout, _dtype_code(W.dtype), W.data_ptr(),
-          _ld(W), strides[0], Q.data_ptr(), _ld(Q), strides[1], S.data_ptr(), _ld(S), strides[2],
-          st)
+    _call(device, agcn_quantize_weight, groups, fin, fout, code, W.data_ptr(), ldw, strides[0],
+          Q.data_ptr(), ldq, strides[1], S.data_ptr(), kb, strides[2], st)
     return Q, S
 
 
@@ -620,71 +635,75 @@ def rms_norm(X, weight, residual=None, eps=1e-6, hidden=None, out=None, stream=N
     X, residual and h are (n, f) of one type (float32, bfloat16 or float16), weight (f,)
     of that type or float32. hidden: where h is written (X or residual itself will
     do); out: a pair (Q, S) to write to."""
-    _check_2d("X", X, getattr(X, "device", None))
-    n, f = X.shape
-    device, dtype = X.device, X.dtype
-    if weight.dim() != 1 or weight.shape[0] != f or (f > 1 and weight.stride(0) != 1):
+    (n, f), device = _first("X", X, 2)
+    dtype, shape = X.dtype, X.shape
+    code, ldx, blocks = _dtype_code("X", dtype), _matrix("X", X, device, shape, dtype), (f + 127) // 128
+    if not isinstance(weight, _torch.Tensor) or weight.device != device:
+        raise TypeError("weight must be a tensor on X's device")
+    g_code = _dtype_code("weight", weight.dtype)
+    if g_code != code and g_code != AGCN_FLOAT:
+        raise TypeError("weight must be float32 or of X's type")
+    if weight.shape != (f,) or (f > 1 and weight.stride(0) != 1):
         raise ValueError("weight must be (f,) and contiguous")
-    if weight.device != device or _dtype_code(weight.dtype) not in (AGCN_FLOAT, _dtype_code(dtype)):
-        raise TypeError("weight must be float32 or of X's type, on X's device")
+    r = h = None
+    ldr = ldh = 0
     if residual is not None:
-        _check_2d("residual", residual, device, (n, f), dtype)
+        ldr = _matrix("residual", residual, device, shape, dtype)
+        r = residual.data_ptr()
+        if hidden is None:
+            hidden, ldh = _new(X, stream, shape, dtype), f
+        else:
+            ldh = _matrix("hidden", hidden, device, shape, dtype)
+        h = hidden.data_ptr()
     elif hidden is not None:
         raise ValueError("hidden needs a residual: without one h is X")
-    if hidden is not None:
-        _check_2d("hidden", hidden, device, (n, f), dtype)
-    more = [((n, f), dtype)] if residual is not None and hidden is None else []
     if out is None:
-        Q, S, *new = _allocate_8bit(device, stream, (n,), f, (n,), *more)
+        Q, ldq = _new_rows(X, stream, (n,), f)
+        S, lds = _new(X, stream, (n, blocks), _S8), blocks
     else:
         Q, S = out
-        _check_8bit(("out[0]", "out[1]"), Q, S, device, (n,), f, (n,))
-        new = _allocate(device, stream, *more)
-    H = new[0] if new else hidden
-    st = _on_stream(device, stream, (X, weight, residual, H, Q, S))
-    r = (None, 0) if residual is None else (residual.data_ptr(), _ld(residual))
-    h = (None, 0) if H is None else (H.data_ptr(), _ld(H))
-    _call(device, agcn_rms_norm, n, f, _dtype_code(dtype), X.data_ptr(), _ld(X), *r, *h,
-          weight.data_ptr(), _dtype_code(weight.dtype), eps, Q.data_ptr(), _ld(Q), S.data_ptr(),
-          _ld(S), st)
-    return (Q, S) if residual is None else (Q, S, H)
+        ldq = _matrix("out[0]", Q, device, shape, _Q8)
+        lds = _matrix("out[1]", S, device, (n, blocks), _S8)
+    st = _on_stream(device, stream, (X, weight, residual, hidden, Q, S))
+    _call(device, agcn_rms_norm, n, f, code, X.data_ptr(), ldx, r, ldr, h, ldh, weight.data_ptr(),
+          g_code, eps, Q.data_ptr(), ldq, S.data_ptr(), lds, st)
+    return (Q, S) if residual is None else (Q, S, hidden)
 
 
 def _product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
-    import torch
-    lead = () if offsets is None else (WQ.shape[0],) if getattr(WQ, "dim", int)() == 3 else (0,)
-    if not isinstance(Q, torch.Tensor) or Q.dim() != 2 or not isinstance(WQ, torch.Tensor) or \
-            WQ.dim() != 2 + len(lead):
-        raise ValueError("Q must be (n, fin) and WQ (fout, fin), or (groups, fout, fin) with "
-                         "offsets")
-    n, fin = Q.shape
-    fout = WQ.shape[-2]
-    device, code = Q.device, _dtype_code(torch.float32 if dtype is None else dtype)
-    _check_8bit(("Q", "S"), Q, S, device, (n,), fin, (n,))
-    _check_8bit(("WQ", "WS"), WQ, WS, device, (*lead, fout), fin, (*lead, (fout + 127) // 128))
-    if code is None:
-        raise TypeError("dtype must be float32, bfloat16 or float16")
-    if act not in _EPILOGUES:
+    shape, device = _first("Q", Q, 2)
+    w_shape, _ = _first("WQ", WQ, 2 if offsets is None else 3)
+    n, fin = shape
+    fout = w_shape[-2]
+    nb, kb = (fout + 127) // 128, (fin + 127) // 128
+    ldq = _matrix("Q", Q, device, shape, _Q8)
+    lds = _matrix("S", S, device, (n, kb), _S8)
+    lead = w_shape[:-2]
+    ldwq = _matrix("WQ", WQ, device, (*lead, fout, fin), _Q8)
+    ldws = _matrix("WS", WS, device, (*lead, nb, kb), _S8)
+    epilogue = _EPILOGUES.get(act)
+    if epilogue is None:
         raise ValueError("act must be None, 'none' or 'relu'")
     if out is None:
-        out, = _allocate(device, stream, ((n, fout), torch.float32 if dtype is None else dtype))
+        dtype = _torch.float32 if dtype is None else dtype
+        code = _dtype_code("the result", dtype)
+        out, ldy = _new(Q, stream, (n, fout), dtype), fout
     else:
-        _check_2d("out", out, device, (n, fout), out.dtype if dtype is None else dtype)
-        code = _dtype_code(out.dtype)
-        if code is None:
-            raise TypeError("out must be float32, bfloat16 or float16")
+        code = _dtype_code("out", getattr(out, "dtype", None))
+        ldy = _matrix("out", out, device, (n, fout), out.dtype if dtype is None else dtype)
     st = _on_stream(device, stream, (Q, S, WQ, WS, offsets, out))
-    a = (Q.data_ptr(), _ld(Q), S.data_ptr(), _ld(S), WQ.data_ptr(), _ld(WQ))
-    y = (code, out.data_ptr(), _ld(out), st, _EPILOGUES[act])
     if offsets is None:
-        _call(device, agcn_quantized_linear, n, fin, fout, *a, WS.data_ptr(), _ld(WS), *y)
+        _call(device, agcn_quantized_linear, n, fin, fout, Q.data_ptr(), ldq, S.data_ptr(), lds,
+              WQ.data_ptr(), ldwq, WS.data_ptr(), ldws, code, out.data_ptr(), ldy, st, epilogue)
         return out
-    if offsets.dtype != torch.int32 or offsets.device != device:
+    groups = lead[0]
+    if offsets.dtype is not _torch.int32 or offsets.device != device:
         raise TypeError("offsets must be int32 on the inputs' device")
-    if tuple(offsets.shape) != (lead[0] + 1,) or (lead[0] > 0 and offsets.stride(0) != 1):
+    if offsets.shape != (groups + 1,) or (groups > 0 and offsets.stride(0) != 1):
         raise ValueError("offsets must be (groups + 1,) and contiguous")
-    _call(device, agcn_grouped_linear, n, fin, fout, lead[0], *a, WQ.stride(0), WS.data_ptr(),
-          _ld(WS), WS.stride(0), offsets.data_ptr(), *y)
+    _call(device, agcn_grouped_linear, n, fin, fout, groups, Q.data_ptr(), ldq, S.data_ptr(), lds,
+          WQ.data_ptr(), ldwq, WQ.stride(0), WS.data_ptr(), ldws, WS.stride(0), offsets.data_ptr(),
+          code, out.data_ptr(), ldy, st, epilogue)
     return out
 
 
@@ -700,6 +719,6 @@ def grouped_linear(Q, S, WQ, WS, offsets, dtype=None, act=None, out=None, stream
     relation): rows offsets[e] to offsets[e + 1] - 1 take WQ[e], WS[e]. offsets: int32 CUDA
     tensor of groups + 1 values that do not decrease, read on the device only; rows
     of no group are 0."""
-    if offsets is None or not hasattr(offsets, "data_ptr"):
+    if not hasattr(offsets, "data_ptr"):
         raise TypeError("offsets must be an int32 CUDA tensor")
     return _product(Q, S, WQ, WS, offsets, dtype, act, out, stream)
