@@ -316,3 +316,87 @@ def test_refusals():
                  lambda: agcn.grouped_linear(Q, S, W3, S3[:1], off)):
         with pytest.raises((TypeError, ValueError)):
             call()
+
+
+# --- each way through the sizes -----------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,fin,fout", [
+    (8200, 1100, 1100), (4200, 1030, 2100), (8192, 1280, 1024), (6000, 1160, 1500),  # 256 x 256 tiles:
+    # whole and partial last blocks of k after odd and even numbers, partial row and column tiles
+    (10000, 200, 1000), (3900, 130, 700), (1500, 200, 1000), (40000, 200, 30),   # smaller tiles
+    (1000, 300, 1000), (1100, 4100, 1200), (500, 1000, 1000), (130, 2000, 900),    # k split over waves
+    (20, 10000, 700)])
+def test_every_tile_shape(n, fin, fout, dtype):
+    Q, S = _rows(n, fin, seed=3)
+    WQ, WS = _weight(fin, fout, seed=3)
+    A, W = values(Q, S), weight_values(WQ, WS)
+    for kind, act in (("padded", "relu"), ("own", None), ("odd", None)):
+        print(f"[linear] {n} x {fin} -> {fout} {dtype} {kind}", flush=True)
+        raw = torch.full((n + 2, fout + 3), 7.0, dtype=TYPES[dtype], device=DEV)
+        got = agcn.quantized_linear(_layout(Q, kind), S, _layout(WQ, kind), WS, act=act,
+                                    out=raw[1:n + 1, 2:fout + 2])
+        _check(got, A, W, dtype, act, fin)
+        raw[1:n + 1, 2:fout + 2] = 7.0
+        assert raw.eq(7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_groups_of_very_different_sizes(dtype):
+    """All rows in one of many groups, where the average group has few; many groups of
+    one row among large ones; large groups beside empty ones."""
+    for n, fin, fout, groups in [(300, 256, 100, 100), (900, 640, 130, 40), (5000, 128, 70, 600)]:
+        for at in (0, groups // 2, groups - 1):
+            off = [0] * (at + 1) + [n] * (groups - at)
+            _check_grouped(n, fin, fout, off, dtype, kind="own")
+            _check_grouped(n, fin, fout, off, dtype, kind="odd", act="relu")
+    sizes = [1] * 70 + [700] + [0] * 5 + [65, 64, 63, 16, 17, 15, 32, 33] + [1] * 50
+    off = [3]
+    for size in sizes:
+        off.append(off[-1] + size)
+    _check_grouped(off[-1] + 9, 300, 100, off, dtype)
+    off = [0, 0, 4000, 4000, 4003, 7900, 7900, 12000]
+    _check_grouped(12000, 1100, 1100, off, dtype, kind="padded")
+    _check_grouped(12000, 1100, 1100, off, dtype, kind="odd", act="relu")
+
+
+def test_more_groups_than_a_grid_has_rows():
+    groups, fin, fout = 66_000, 32, 8
+    Q, S = _rows(groups, fin)
+    WQ, WS = _weight(fin, fout, (groups,))
+    off = torch.arange(groups + 1, dtype=torch.int32, device=DEV)
+    got = agcn.grouped_linear(Q, S, WQ, WS, off)
+    A, W = values(Q, S), weight_values(WQ, WS)
+    Y, T = (W @ A[:, :, None])[..., 0], (W.abs() @ A.abs()[:, :, None])[..., 0]
+    assert bool(((got.double() - Y).abs() <= _bound(Y, T, "float32", fin)).all())
+
+
+def test_every_scale_code():
+    """Codes 0 to 255 of A with 254 - code of W: the product of the scales is 1, and NaN
+    with 255. Values that bf16 holds (down to 2^-133) come out exactly scaled."""
+    code = torch.arange(256, device=DEV)
+    Q = torch.full((256, 128), 1.5, device=DEV).to(torch.float8_e4m3fn)
+    S = code.to(torch.uint8)[:, None].contiguous().view(torch.float8_e8m0fnu)
+    WQ = torch.zeros((256 * 128, 128), device=DEV)
+    WQ[::128, 7] = 1
+    WQ = WQ.to(torch.float8_e4m3fn)
+    WS = (254 - code).clamp(min=0).to(torch.uint8)[:, None].contiguous().view(torch.float8_e8m0fnu)
+    for dtype in ("float32", "bfloat16"):
+        Y = agcn.quantized_linear(Q, S, WQ, WS, dtype=TYPES[dtype])[:, ::128]
+        d = Y.diagonal()
+        assert d[:255].float().eq(1.5).all() and torch.isnan(d[255])
+        assert torch.isnan(Y[255]).all()
+
+
+def test_rows_of_zeros_beside_others():
+    """Blocks of zeros have the least scale."""
+    x = torch.randn((300, 256), generator=_gen(5), device=DEV)
+    x[::7] = 0
+    x[3, 128:] = 0
+    Q, S = agcn.quantize(x)
+    WQ, WS = _weight(256, 90)
+    for dtype in sorted(TYPES):
+        got = agcn.quantized_linear(Q, S, WQ, WS, dtype=TYPES[dtype])
+        assert got[::7].eq(0).all()
+        _check(got, values(Q, S), weight_values(WQ, WS), dtype, None, 256)
