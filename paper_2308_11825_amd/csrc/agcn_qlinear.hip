@@ -9,10 +9,9 @@
 // bits its sums are off by 1.4e-5 (2-norm, normal values, K = 128 to 4096; 5e-5 where
 // all bit patterns are equally likely), a hundredth of the rounding to
 // bfloat16 (1.7e-3) and less than a tenth of that to float16 (2.1e-4): those
-// outputs are computed with it. For float32 outputs the values are turned into
-// bf16, which holds every e4m3 value, and multiplied on the bf16 matrix cores
-// from zero for each block; the block's sum is scaled and added in fp32:
-// 8e-8 at K = 4096.
+// outputs are computed with it. For float32 outputs the values times their scales
+// are turned into bf16, which holds them exactly, and multiplied on the bf16 matrix
+// cores: 8e-8 at K = 4096, for twice the time (4096 x 4096 -> 4096 60 us and 128).
 //
 // W's rows are the instruction's rows and A's its columns: a lane then holds
 // four neighbouring outputs of one row of Y, and the scale of one row of A.
@@ -378,9 +377,10 @@ struct Stage {
   }
 };
 
-// Half of a 256-row tile for 4 waves: of every 128 rows those of half `h`.
-template <int PERM>
+// Half of a tile of 4 H rows for 4 waves: of every 2 H rows H from `h` H on.
+template <int H, int PERM>
 struct HalfStage {
+  static constexpr int kSteps = 2 * H / 32;
   const uint8_t* base;
   uint32_t bytes, first;
   int32_t ld, piece;
@@ -396,14 +396,15 @@ struct HalfStage {
   static __device__ __forceinline__ int place(int i, int wave) { return (i * 4 + wave) * 1024; }
   __device__ __forceinline__ void issue(uint8_t* lds, uint32_t k, int h, int i, int wave) const {
     const auto res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+    const int row = i * 32 / H * 2 * H + i * 32 % H + h * H;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         res, (__attribute__((address_space(3))) void*)(lds + place(i, wave)), 16,
-        first + ((uint32_t)((i / 2 * 128 + i % 2 * 32 + h * 64) * ld) + k), 0, 0, 0);
+        first + ((uint32_t)(row * ld) + k), 0, 0, 0);
   }
   __device__ __forceinline__ void mask(uint8_t* lds, int left, int wave, int lane) const {
     const v4i keep = bytes_kept(left - piece);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16) &= keep;
+    for (int i = 0; i < kSteps; ++i) *reinterpret_cast<v4i*>(lds + place(i, wave) + lane * 16) &= keep;
   }
 };
 
@@ -481,7 +482,8 @@ __device__ __forceinline__ void write_tile(bool whole, int32_t act, F write) {
 
 // BM x BN outputs per workgroup of WM x WN waves, TM x TN a wave, one block of 128 k
 // at a time: while the waves multiply one block from LDS, the next is on its way
-// into the other half.
+// into the other half. For outputs too narrow or too few for k_qlinear_ring, where the
+// time is memory's or the latency of the loads: 230,000 x 128 -> 41 13.5 us, 3.6 TB/s.
 template <int TM, int TN, int WM, int WN, bool EXACT, class TY, bool GROUPED, bool ASYNC>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, uint32_t tiles_n,
                                                                uint32_t group_m) {
@@ -710,19 +712,24 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_stream(LinearArgs p) {
   }
 }
 
-// 256 x 256 outputs per workgroup of 4 waves, 128 x 128 a wave: the accumulators fill
-// half of the registers and one wave a SIMD is left, so nothing but the order of its
-// own instructions hides LDS and memory. A block of 128 k is multiplied in four
-// quarters of 64 x 64, and a quarter needs one new half of A or W, which is read from LDS
-// during the quarter before:
+// 4 H x 4 H outputs per workgroup of 4 waves, 2 H x 2 H a wave. With H = 64 the
+// accumulators fill half of the registers and one wave a SIMD is left, so nothing but the
+// order of its own instructions hides LDS and memory. A block of 128 k is multiplied in
+// four quarters of H x H, and a quarter needs one new half of A or W, which is read
+// from LDS during the quarter before:
 //   A0 W0 | read W1,   A0 W1 | read A1,   A1 W1 | read A0',   A1 W0 | read W1'
 // (' the next block, which starts with the other half of W). So LDS is filled and
-// emptied in halves of a block, of A and of W together: five slots of 32 KB, one being
-// read and four on their way, which are two blocks' time to arrive.
-template <class TY, bool GROUPED>
-__global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t tiles_n,
-                                                        uint32_t group_m) {
-  constexpr int BM = 256, BN = 256, kSlots = 5, kSlot = 256 * kQBlock, kPart = 128 * kQBlock;
+// emptied in halves of a block, of A and of W together: five slots (32 KB each, or 16 KB and
+// two workgroups a compute unit), one being read and four on their way, which are
+// two blocks' time to arrive. EXACT: a half becomes bf16 when it has been read.
+// H = 64: 4096 x 4096 -> 4096 58 us, 16384 x 8192 -> 8192 850 us, 2.4 and 2.6 PFLOP/s, where the chip
+// lowers its clock to about 2 GHz. H = 32: 16384 x 1024 -> 4096 75 us, 1.8 PFLOP/s, bound by LDS;
+// 230,000 x 128 -> 128 17 us, 5.1 TB/s.
+template <int H, bool EXACT, class TY, bool GROUPED>
+__global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArgs p, uint32_t tiles_n,
+                                                                       uint32_t group_m) {
+  constexpr int BM = 4 * H, BN = 4 * H, T = H / 32, kSlots = 5, kPart = 2 * H * kQBlock, kSlot = 2 * kPart;
+  constexpr int kLoads = H / 8, kCodes = 2 * T + 1;  // a wave's loads of half a block, and of scales
   __shared__ __align__(1024) uint8_t lds[kSlots * kSlot];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane % 32, g = lane / 32, wm = wave % 2, wn = wave / 2;
@@ -730,54 +737,55 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
   const Rows rows = tile_rows<BM, GROUPED>(p, tiles_n, group_m, &tn);
   if (rows.count <= 0) return;
   const int n0 = (int)tn * BN, count_n = min(BN, p.fout - n0);
-  v16f acc[4][4];
+  v16f acc[2 * T][2 * T];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 2 * T; ++j)
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 2 * T; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[j][t][i] = 0.0f;
 
   const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
   if (blocks > 0) {
-    // Two blocks a round; an odd number starts with one of zeros, so that the last
-    // block, which may be a part of one, always comes second in the last round.
-    const int none = blocks & 1, total = blocks + none;
-    HalfStage<0> sa;
-    HalfStage<32> sw;
+    // Two blocks a round; an odd number starts with a round's second, so that the last
+    // block, which may be a part of one, always comes second in the last round. (H = 64
+    // has no registers for a way into the middle and takes a block of zeros first.)
+    constexpr bool kSkip = H < 64;
+    const int none = blocks & 1, total = blocks + none, begin = kSkip ? none : 0;
+    HalfStage<H, 0> sa;
+    HalfStage<H, 32> sw;
     sa.init(p.A + rows.row * p.lda, p.lda, rows.count, p.fin, wave, lane);
     sw.init(p.W + rows.group * p.group_w + (int64_t)n0 * p.ldw, p.ldw, count_n, p.fin, wave, lane);
     RowScales<32> scale_a;
-    scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * 128 + r);
+    scale_a.init(p.SA + rows.row * p.ldsa, p.ldsa, rows.count, blocks, wm * 2 * H + r);
     const uint8_t* scale_w =
         p.SW + rows.group * p.group_sw +
-        (int64_t)min((n0 + wn * 128) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
+        (int64_t)min((n0 + wn * 2 * H) / kQBlock, (p.fout - 1) / kQBlock) * p.ldsw;
     // Fragments: pieces g, g + 2 (the first 64 k), g + 4 and g + 6 of a row.
     const int row_w = r / 16 * 16 + r / 4 % 2 * 8 + r / 8 % 2 * 4 + r % 4;
-    const int frag_a = (wm * 64 + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
-    const int frag_w = kPart + (wn * 64 + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
+    const int frag_a = (wm * H + r) * kQBlock + ((g ^ swizzle_key<0>(r)) * 16);
+    const int frag_w = kPart + (wn * H + row_w) * kQBlock + ((g ^ swizzle_key<32>(row_w)) * 16);
 
-    uint32_t code_a[4], next_a[2][4], code_w, next_w[2];
+    uint32_t code_a[2 * T], next_a[2][2 * T], code_w, next_w[2];
     int to = 0, from = 0;  // slots to fill and to read next
     auto advance = [](int& slot) { slot = slot == (kSlots - 1) * kSlot ? 0 : slot + kSlot; };
-    // Half h of block i: rows 64 h to 64 h + 63 of every 128 of A, and of W the other
-    // half in odd blocks. Past the last block nothing is read (zeros arrive).
-    // Load l of a wave's 8.
+    // Load l of a wave's for half h of block i: rows H h on of every 2 H of A, and of W the
+    // other half in odd blocks. Past the last block nothing is read (zeros arrive).
     auto issue = [&](int i, int h, int l) {
       const uint32_t k = i < total ? (uint32_t)((i - none) * kQBlock) : 0x80000000u;
-      if (l < 4) sa.issue(lds + to, k, h, l, wave);
-      else sw.issue(lds + to + kPart, k, h ^ (i & 1), l - 4, wave);
-      if (l == 7) advance(to);
+      if (l < kLoads / 2) sa.issue(lds + to, k, h, l, wave);
+      else sw.issue(lds + to + kPart, k, h ^ (i & 1), l - kLoads / 2, wave);
+      if (l == kLoads - 1) advance(to);
     };
     auto issue_all = [&](int i, int h) {
 #pragma unroll
-      for (int l = 0; l < 8; ++l) issue(i, h, l);
+      for (int l = 0; l < kLoads; ++l) issue(i, h, l);
     };
     // Two blocks ahead: loads arrive in their order, and a block's scales are asked for
     // after the values of the first half of the block after the next.
     auto code = [&](int i, int u, int l) {
       const int b = min(max(i - none, 0), blocks - 1);
-      if (l < 4) next_a[u][l] = scale_a.load(l, b);
+      if (l < 2 * T) next_a[u][l] = scale_a.load(l, b);
       else next_w[u] = scale_w[b];
     };
     auto mask = [&](int slot, int left) {
@@ -785,130 +793,179 @@ __global__ __launch_bounds__(256, 1) void k_qlinear_big(LinearArgs p, uint32_t t
       sw.mask(lds + slot + kPart, left, wave, lane);
     };
     // The half at `from` is in LDS and the one before it has been read, by all waves.
-    // A half is 8 loads a wave, and three younger ones may be on their way.
-    auto arrive = [&](int left) {
-      asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+    // `young` later ones have been asked for and may be on their way.
+    auto arrive = [&](int left, auto young) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(young)::value * kLoads) : "memory");
       if (left < kQBlock) mask(from, left);
       // (A fence would wait for every load into LDS.)
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
-    v8i a0[4], a1[4], w0[4], w1[4];  // 2 * half of 64 k + tile of 32 rows
-    auto read = [&](v8i (&v)[4], int at, int c) {
-      const int x = at + c % 2 * 32 * kQBlock, h = c / 2 * 64;
-      v[c] = join(*reinterpret_cast<const v4i*>(lds + from + (x ^ h)),
-                  *reinterpret_cast<const v4i*>(lds + from + (x ^ (h + 32))));
+    // Half an operand: [64 k][tile of 32 rows], as read and as multiplied.
+    struct Half {
+      v8i q[2 * T];
+      v8b b[EXACT ? 2 * T : 1][EXACT ? 4 : 1];
     };
-    // A quarter: eight products, and after the k-th what `between` issues in its shadow.
-    auto quarter = [&](const v8i (&w)[4], const v8i (&a)[4], int hw, int ha, auto between) {
+    Half a0, a1, w0, w1;
+    auto read = [&](Half& v, int at, int c) {
+      const int x = at + c % T * 32 * kQBlock, h = c / T * 64;
+      v.q[c] = join(*reinterpret_cast<const v4i*>(lds + from + (x ^ h)),
+                    *reinterpret_cast<const v4i*>(lds + from + (x ^ (h + 32))));
+    };
+    auto convert = [&](Half& v, const uint32_t* scale, int step) {
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int c = 0; c < 2 * T; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v.b[c][i] = to_bf16(v.q[c], i, scale[c % T * step]);
+      }
+    };
+    // A quarter in eight parts, and after each what `between` issues in its shadow.
+    auto quarter = [&](const Half& w, const Half& a, int hw, int ha, auto between) {
+      constexpr int kProducts = T * T * 2 * (EXACT ? 4 : 1);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int h = k / 4, j = k / 2 % 2, t = k % 2;
-        v16f& c = acc[hw * 2 + j][ha * 2 + t];
-        c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[2 * h + j], a[2 * h + t], c, 0, 0, 0,
-                                                            (int)code_w, 0, (int)code_a[ha * 2 + t]);
+#pragma unroll
+        for (int x = k * kProducts / 8; x < (k + 1) * kProducts / 8; ++x) {
+          const int j = x / T % T, t = x % T, y = x / (T * T);  // y: the step of k
+          v16f& c = acc[hw * T + j][ha * T + t];
+          if constexpr (EXACT)
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.b[y / 4 * T + j][y % 4], a.b[y / 4 * T + t][y % 4], c,
+                                                        0, 0, 0);
+          else
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.q[y * T + j], a.q[y * T + t], c, 0, 0, 0,
+                                                                (int)code_w, 0, (int)code_a[ha * T + t]);
+        }
         between(k);
-        __builtin_amdgcn_sched_barrier(0);
+        if (H == 64) __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_sched_barrier(0);
     };
     // Block i, its first half of W (number `first`) in wf; the other goes to wo. WHICH: 0 a
     // block in the middle, 1 the one before the last, 2 the last.
-    auto step = [&](int i, int first, v8i (&wf)[4], v8i (&wo)[4], auto which) {
+    auto step = [&](int i, int first, Half& wf, Half& wo, auto which) {
       constexpr int WHICH = decltype(which)::value;
       const int left = WHICH == 0 ? kQBlock : p.fin - (blocks - 1) * kQBlock;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) code_a[t] = next_a[first][t];
+      for (int t = 0; t < 2 * T; ++t) code_a[t] = next_a[first][t];
       code_w = next_w[first];
       // At most one load after a product: the four waves' loads are taken in turn.
+      convert(wf, &code_w, 0);
+      convert(a0, code_a, 1);
       quarter(wf, a0, first, 0, [&](int k) {
-        if (k == 0) arrive(WHICH == 2 ? left : kQBlock);
-        else if (k <= 4) read(wo, frag_w, k - 1);
-        if (WHICH == 2) return;
-        if (k >= 1 && k < 6) code(i + 2, first, k - 1);
-        if (k >= 6) issue(i + 2, 1, k - 6);
+        if (k == 0) arrive(WHICH == 2 ? left : kQBlock, std::integral_constant<int, WHICH == 2 ? 1 : 3>{});
+        else if (k <= 2 * T) read(wo, frag_w, k - 1);
+        if (WHICH > 0) return;
+        if (k >= 1 && k <= kCodes) code(i + 2, first, k - 1);
+        if (k >= 6 && k - 6 < kLoads) issue(i + 2, 1, k - 6);
       });
+      convert(wo, &code_w, 0);
       quarter(wo, a0, 1 - first, 0, [&](int k) {
-        if (k < 4) read(a1, frag_a, k);
+        if (k < 2 * T) read(a1, frag_a, k);
         if (k == 4) advance(from);
-        if (k >= 2 && WHICH < 2) issue(i + 2, 1, k);
+        if (k >= 2 && k < kLoads && WHICH == 0) issue(i + 2, 1, k);
       });
+      convert(a1, code_a + T, 1);
       quarter(wo, a1, 1 - first, 1, [&](int k) {
         if (WHICH == 2) return;
-        if (k == 0) arrive(WHICH == 1 ? left : kQBlock);
-        else if (k <= 4) read(a0, frag_a, k - 1);
-        if (k >= 5) issue(i + 3, 0, k - 5);
+        if (k == 0) arrive(WHICH == 1 ? left : kQBlock, std::integral_constant<int, WHICH == 1 ? 2 : 3>{});
+        else if (k <= 2 * T) read(a0, frag_a, k - 1);
+        if (k >= 5 && k - 5 < kLoads && WHICH == 0) issue(i + 3, 0, k - 5);
       });
       quarter(wf, a1, first, 1, [&](int k) {
         if (WHICH == 2) return;
-        if (k < 4) read(wo, frag_w, k);
+        if (k < 2 * T) read(wo, frag_w, k);
         if (k == 4) advance(from);
-        if (k >= 3) issue(i + 3, 0, k);
+        if (k >= 3 && k < kLoads && WHICH == 0) issue(i + 3, 0, k);
       });
     };
-    if (none) {
+    if (!kSkip && none) {
       mask(0, 0);
       mask(kSlot, 0);
       to = 2 * kSlot;
     } else {
-      issue_all(0, 0);
-      issue_all(0, 1);
+      issue_all(begin, 0);
+      issue_all(begin, 1);
     }
-    issue_all(1, 0);
-    issue_all(1, 1);
+    const bool one = kSkip && blocks == 1;
+    if (!one) {
+      issue_all(begin + 1, 0);
+      issue_all(begin + 1, 1);
+    }
 #pragma unroll
-    for (int l = 0; l < 10; ++l) code(l / 5, l / 5, l % 5);
-    arrive(kQBlock);
+    for (int l = 0; l < 2 * kCodes; ++l) code(l / kCodes, l / kCodes, l % kCodes);
+    if (one) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    arrive(one ? p.fin : kQBlock, std::integral_constant<int, 2>{});
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < 2 * T; ++c) {
       read(a0, frag_a, c);
       read(w0, frag_w, c);
+      if (kSkip) read(w1, frag_w, c);
     }
-    issue_all(2, 0);
+    if (!one) issue_all(begin + 2, 0);
     advance(from);
+    using Middle = std::integral_constant<int, 0>;
+    using Before = std::integral_constant<int, 1>;
+    using Last = std::integral_constant<int, 2>;
     int i = 0;
-    for (; i + 2 < total; i += 2) {
-      step(i, 0, w0, w1, std::integral_constant<int, 0>{});
-      step(i + 1, 1, w1, w0, std::integral_constant<int, 0>{});
+    if (one) {
+      step(1, 1, w1, w0, Last{});
+    } else {
+      if (kSkip && none) {
+#pragma unroll
+        for (int l = 0; l < kCodes; ++l) code(2, 0, l);
+        step(1, 1, w1, w0, Middle{});
+        i = 2;
+      }
+      for (; i + 2 < total; i += 2) {
+        step(i, 0, w0, w1, Middle{});
+        step(i + 1, 1, w1, w0, Middle{});
+      }
+      step(i, 0, w0, w1, Before{});
+      step(i + 1, 1, w1, w0, Last{});
     }
-    step(i, 0, w0, w1, std::integral_constant<int, 1>{});
-    step(i + 1, 1, w1, w0, std::integral_constant<int, 2>{});
     __builtin_amdgcn_s_waitcnt(0);  // what was fetched past the last block
   }
   // 32 rows at a time through the wave's own part of LDS, so that 16 lanes write 256
   // neighbouring bytes of Y (a lane's own 16 bytes of 32 rows made 3 TB/s of the
   // whole chip's writes). Rows are 16 bytes apart from a multiple of the banks.
   __syncthreads();
-  constexpr int kRow = 128 * sizeof(TY) + 16;
+  constexpr int kRun = 16 / sizeof(TY), kRow = 2 * H * sizeof(TY) + 16, kLanes = 2 * H / kRun;
   uint8_t* own = lds + wave * 32 * kRow;
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
   write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
     constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
     struct alignas(16) Run {
-      TY e[8];
+      TY e[kRun];
     };
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < 2 * T; ++t) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 2 * T; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int c = 0; c < 16; c += kRun) {
           Run v;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v.e[i] = (TY)q_act(acc[j][t][8 * h + i], RELU);
-          *reinterpret_cast<Run*>(own + r * kRow + (j * 32 + 16 * h + 8 * g) * sizeof(TY)) = v;
+          for (int i = 0; i < kRun; ++i) v.e[i] = (TY)q_act(acc[j][t][c + i], RELU);
+          *reinterpret_cast<Run*>(own + r * kRow + (j * 32 + c / 8 * 16 + 8 * g + c % 8) * sizeof(TY)) = v;
         }
+      const int n = lane % kLanes * kRun, left = count_n - wn * 2 * H - n, row0 = wm * 2 * H + t * 32 + lane / kLanes;
+      TY* to = y + row0 * p.ldy + wn * 2 * H + n;
+      auto each = [&](auto store) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = i * 4 + lane / 16, m = wm * 128 + t * 32 + row, n = wn * 128 + lane % 16 * 8;
-        const Run v = *reinterpret_cast<const Run*>(own + row * kRow + lane % 16 * 16);
-        if (!ALL && m >= rows.count) continue;
-        TY* to = y + m * p.ldy + n;
-        if (ALL || n + 8 <= count_n) {
-          store_any(to, v);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (n + k < count_n) to[k] = v.e[k];
+        for (int i = 0; i < kLanes / 2; ++i) {
+          const int m = i * (64 / kLanes);
+          const Run v = *reinterpret_cast<const Run*>(own + (m + lane / kLanes) * kRow + lane % kLanes * 16);
+          if (ALL || row0 + m < rows.count) store(to + m * p.ldy, v);
         }
+      };
+      if (ALL || left >= kRun) {
+        each([](TY* at, const Run& v) { store_any(at, v); });
+      } else if (left > 0) {
+        each([&](TY* at, const Run& v) {
+#pragma unroll
+          for (int k = 0; k < kRun; ++k)
+            if (k < left) at[k] = v.e[k];
+        });
       }
     }
   });
@@ -941,13 +998,13 @@ int launch_tile(const LinearArgs& p, hipStream_t st) {
   return launched("k_qlinear_tile launch");
 }
 
-template <class TY, bool GROUPED>
-int launch_big(const LinearArgs& p, hipStream_t st) {
-  const TileGrid t = tile_grid<256, 256, GROUPED>(p);
+template <int H, bool EXACT, class TY, bool GROUPED>
+int launch_ring(const LinearArgs& p, hipStream_t st) {
+  const TileGrid t = tile_grid<4 * H, 4 * H, GROUPED>(p);
   if (t.tiles > kMostTiles) return fail(AGCN_ERR_UNSUPPORTED, "matrix too large for one launch");
-  k_qlinear_big<TY, GROUPED>
+  k_qlinear_ring<H, EXACT, TY, GROUPED>
       <<<(unsigned)t.tiles, 256, 0, st>>>(p, (uint32_t)t.tiles_n, (uint32_t)t.group_m);
-  return launched("k_qlinear_big launch");
+  return launched("k_qlinear_ring launch");
 }
 
 template <int MT, int U, bool EXACT, class TY, bool GROUPED>
@@ -966,8 +1023,8 @@ int launch_stream(const LinearArgs& p, hipStream_t st) {
   return launched("k_qlinear_stream launch");
 }
 
-// Which kernel. Figures are us on one MI355X, bfloat16 outputs; the float32 ones, without
-// k_qlinear_big, cross at the same places.
+// Which kernel. Figures are us on one MI355X, bfloat16 outputs; k_qlinear_ring by its H,
+// k_qlinear_tile by its outputs.
 template <bool EXACT, class TY, bool GROUPED>
 int linear_typed(const LinearArgs& p, hipStream_t st) {
   constexpr int64_t kUnits = 256;  // compute units
@@ -994,39 +1051,51 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
   }
   if constexpr (GROUPED) {
     // Few rows a group: bound by the weights, which are read once per row tile. 512 x 4096
-    // -> 2048 over 64 groups 93 with 32 x 32 outputs, 99 with 64 x 64 and 148 in k_qlinear_tile;
-    // 2048 rows 151, 125 and 155; 4096 rows 236, 169 and 164 (k_qlinear_big).
+    // -> 2048 over 64 groups 93 with 32 x 32 outputs, 99 with 64 x 64; 2048 rows 151, 117 and
+    // 130 in k_qlinear_ring<32>; 4096 rows 236, 159 and 148.
     if (fits_y && rows <= 12) return launch_stream<2, 2, 4, 2, EXACT, TY, true>(p, st);
     if (fits_y && rows < 64) return launch_stream<4, 4, 4, 1, EXACT, TY, true>(p, st);
   } else if (tiles(64, 64) <= kUnits) {
     // Few outputs: the largest tile of which there are not more than compute units, each
     // read by a workgroup that splits k over its waves. 16, 64, 128 and 256 x 4096 -> 4096:
     // 6.6, 11.2, 19.8, 36 with 16 x 32 outputs; 7.2, 8.5, 13.2, 22 with 32 x 32; 8.6, 10.0, 10.9,
-    // 18 with 32 x 64; 10.7, 13.7, 13.9, 14.5 with 64 x 64; k_qlinear_tile 20 to 24.
+    // 18 with 32 x 64; 10.7, 13.7, 13.9, 14.5 with 64 x 64; 2048 x 4096 -> 512 18.1, ring<32> 20.1.
+    // A short k has too few blocks to split: 4096 x 256 -> 256 6.8 in 64 x 64 outputs, 4.3 in
+    // k_qlinear_tile's; 1024 x 1024 -> 1024 7.1 and 6.2; 1024 x 2048 -> 1024 9.6 and 9.0, float32 11.5 and 11.9.
     if (tiles(16, 32) <= kUnits) return launch_stream<1, 2, 8, 2, EXACT, TY, false>(p, st);
     if (tiles(32, 32) <= kUnits) return launch_stream<2, 2, 4, 2, EXACT, TY, false>(p, st);
     if (tiles(32, 64) <= kUnits) return launch_stream<2, 4, 4, 2, EXACT, TY, false>(p, st);
+    if (p.fin < 2048) return launch_tile<32, 32, 2, 2, EXACT, TY, false, true>(p, st);
     return launch_stream<4, 4, 4, 2, EXACT, TY, false>(p, st);
-  } else if (tiles(64, 64) <= 2 * kUnits && p.fin >= 4096) {
-    // Two workgroups a compute unit and a long k: 512 x 4096 -> 4096 22.5, k_qlinear_tile 25;
-    // 1024 x 2048 -> 2048 13.5 and 12.9.
-    return launch_stream<4, 4, 4, 1, EXACT, TY, false>(p, st);
   }
-  // The matrix cores bound it from half a tile per compute unit on: 2048 x 4096 -> 4096 47, 55 in
-  // tiles of 128; 1024 x 4096 -> 4096 42 and 34. Short k end before its loads are under way
-  // (65536 x 512 -> 512 31 and 32), and half-empty column tiles cost what full ones do (65536 x
-  // 1024 -> 128 30 and 18).
-  if constexpr (!EXACT)
-    if (rows >= 256 && p.fin >= 1024 && tiles(256, 256) >= kUnits / 2 &&
-        tiles(256, 256) * 16 <= tiles(128, 128) * 5)
-      return launch_big<TY, GROUPED>(p, st);
+  // A full chip and a long k: half the reads of LDS and cache per product. 4096 x 4096 -> 4096
+  // ring<64> 60 and ring<32> 81; 8192 x 2048 -> 2048 36 and 38; 65536 x 1536 -> 512 57 and 66. Short k
+  // end before its loads are under way, unless there are few columns and A is most
+  // of the reading: 65536 x 512 -> 512 37 and 28; 16384 x 1024 -> 4096 88 and 79; 65536 x 1024 -> 512 46
+  // and 41; 230,000 x 602 -> 256 84 and 93, x 1024 100 and 105, x 512 73 and 63. Half a tile per compute
+  // unit is too few (2048 x 4096 -> 4096 48 and 43), and half-empty column tiles cost what
+  // full ones do (230,000 x 200 -> 200 51 and 40).
+  if constexpr (!EXACT) {
+    const int64_t large = tiles(256, 256);
+    if (rows >= 256 && large >= kUnits && large * 16 <= tiles(128, 128) * 5 &&
+        (p.fin >= 1536 || (p.fin > 512 && p.fout <= 512 && large > 3 * kUnits)))
+      return launch_ring<64, false, TY, GROUPED>(p, st);
+  }
   // Narrow outputs fill narrow tiles: 230,000 x 128 -> 41 13.7 with 64 columns, 22.5 with 128;
   // 230,000 x 256 -> 16 13.6 with 32 columns, 16.8 with 64.
   if (p.fout <= 32 && tiles(128, 32) >= kUnits) return launch_tile<32, 32, 4, 1, EXACT, TY, GROUPED, true>(p, st);
-  // Large tiles read less, small ones fill the chip: 16384 x 512 -> 512 (512 tiles of 128)
-  // 11.6, 13.0 with 128 x 64; 4096 x 1024 -> 1024 11.7 and 11.3; 1024 x 2048 -> 2048 17.1, 14.6 and 12.9 with
-  // 64 x 64.
-  if (p.fout > 64 && tiles(128, 128) >= 2 * kUnits) return launch_tile<64, 64, 2, 2, EXACT, TY, GROUPED, true>(p, st);
+  // Half a tile per compute unit is enough where the loads bound it, and one where the
+  // conversions do. ring<32> and the smaller tile: 512 x 4096 -> 4096 21.5 and 23.4
+  // (k_qlinear_stream); 1024 x 2048 -> 2048 11.6 and 12.8 (64 x 64); 16384 x 512 -> 512 10.8 and 13.0 (128 x
+  // 64); 4096 x 1024 -> 1024 9.2 and 11.3. float32: 512 x 4096 -> 4096 33.4 and 25.6 (stream), 1024 x 2048
+  // -> 2048 19.4 and 15.6.
+  if (p.fout > 64 && tiles(128, 128) >= (EXACT ? kUnits : kUnits / 2))
+    return launch_ring<32, EXACT, TY, GROUPED>(p, st);
+  // Two workgroups a compute unit, each wave with blocks of its own.
+  if constexpr (!GROUPED)
+    if (tiles(64, 64) <= 2 * kUnits && p.fin >= (EXACT ? 2048 : 4096))
+      return launch_stream<4, 4, 4, 1, EXACT, TY, false>(p, st);
+  // 65536 x 602 -> 64 12.2 in 128 x 64 outputs; 2000 x 512 -> 512 over 8 groups 6.6.
   if (tiles(128, 64) > kUnits) return launch_tile<32, 64, 4, 1, EXACT, TY, GROUPED, true>(p, st);
   return launch_tile<32, 32, 2, 2, EXACT, TY, GROUPED, true>(p, st);
 }

@@ -343,6 +343,35 @@ def test_every_tile_shape(n, fin, fout, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,fin,fout", [
+    (4090, 1700, 4000), (8300, 1550, 2050), (8192, 1664, 2048), (200_000, 600, 250),  # 256 x 256
+    (40_000, 100, 300), (40_000, 16, 100), (40_000, 256, 128), (40_000, 270, 200),  # 128 x 128
+    (900, 3000, 1000), (4000, 250, 250)])  # few: k split over waves, a short k not
+def test_large_tiles(n, fin, fout, dtype):
+    """Whole and partial last blocks of k after odd and even numbers of blocks, one block
+    alone, partial row and column tiles."""
+    Q, S = _rows(n, fin, seed=5)
+    WQ, WS = _weight(fin, fout, seed=5)
+    A, W = values(Q, S), weight_values(WQ, WS)
+    for act in (None, "relu"):
+        print(f"[linear] {n} x {fin} -> {fout} {dtype} {act}", flush=True)
+        raw = torch.full((n + 2, fout + 3), 7.0, dtype=TYPES[dtype], device=DEV)
+        got = agcn.quantized_linear(_layout(Q, "padded"), S, _layout(WQ, "padded"), WS, act=act,
+                                    out=raw[1:n + 1, 2:fout + 2])
+        _check(got, A, W, dtype, act, fin)
+        raw[1:n + 1, 2:fout + 2] = 7.0
+        assert raw.eq(7.0).all()
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_large_tiles_of_groups(dtype):
+    off = [0, 0, 4000, 4000, 4003, 7900, 7900, 11_990]
+    _check_grouped(12_000, 1600, 1600, off, dtype, kind="padded", act="relu")
+    _check_grouped(12_000, 1540, 1601, off, dtype, kind="padded")
+    _check_grouped(12_000, 90, 700, off, dtype, kind="padded")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_groups_of_very_different_sizes(dtype):
     """All rows in one of many groups, where the average group has few; many groups of
     one row among large ones; large groups beside empty ones."""
