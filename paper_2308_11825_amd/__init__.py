@@ -585,8 +585,12 @@ def _new(like, stream, shape, dtype):
 
 
 def _new_rows(like, stream, lead, k):
-    """Values (..., k) in 8 bits with rows that start on 16 bytes, and their row stride."""
-    ld = (k + 15) // 16 * 16
+    """Values (..., k) in 8 bits and their row stride: rows start on 16 bytes, on 128 (the
+    lines of memory, which a block of 128 columns then is one of) where that adds an
+    eighth at most: 230,000 x 602 -> 256 bfloat16 75 us with rows of 640 bytes, 90 with 608."""
+    ld = (k + 127) // 128 * 128
+    if ld > k + k // 8:
+        ld = (k + 15) // 16 * 16
     q = _new(like, stream, (*lead, ld), _Q8)
     return (q[..., :k] if k != ld else q), ld
 
