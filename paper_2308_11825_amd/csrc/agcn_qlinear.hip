@@ -27,6 +27,7 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef v4f v4f_any __attribute__((aligned(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
@@ -927,7 +928,10 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
   }
   // 32 rows at a time through the wave's own part of LDS, so that 16 lanes write 256
   // neighbouring bytes of Y (a lane's own 16 bytes of 32 rows made 3 TB/s of the
-  // whole chip's writes). Rows are 16 bytes apart from a multiple of the banks.
+  // whole chip's writes). Rows are 16 bytes apart from a multiple of the banks. float32 is
+  // written past L2, which then keeps A's rows for the other column tiles: 230,000 x 602 ->
+  // 256 122 us, otherwise 134; 16384 x 1024 -> 4096 149 and 159. bfloat16 gains as often as it loses
+  // (78 and 83; 82 and 75).
   __syncthreads();
   constexpr int kRun = 16 / sizeof(TY), kRow = 2 * H * sizeof(TY) + 16, kLanes = 2 * H / kRun;
   uint8_t* own = lds + wave * 32 * kRow;
@@ -959,7 +963,10 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
         }
       };
       if (ALL || left >= kRun) {
-        each([](TY* at, const Run& v) { store_any(at, v); });
+        each([](TY* at, const Run& v) {
+          if constexpr (EXACT) __builtin_nontemporal_store(__builtin_bit_cast(v4f, v), (v4f_any*)at);
+          else store_any(at, v);
+        });
       } else if (left > 0) {
         each([&](TY* at, const Run& v) {
 #pragma unroll
