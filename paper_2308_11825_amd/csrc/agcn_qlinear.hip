@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "agcn_quant.hpp"
+#include "agcn_row_tiles.hpp"
 
 namespace agcn {
 
@@ -125,97 +126,6 @@ __device__ __forceinline__ void block_products(v4f (&acc)[NT][MT], GetW w, GetA 
   }
 }
 
-// The rows a tile of at most BM rows works on: rows [row, row + count) of group
-// `group`, or rows of no group (group -1), which are set to 0.
-struct Rows {
-  int64_t row;
-  int32_t count, group;
-};
-
-// The rows cut at the groups' offsets, in tiles of BM. The rows before the first
-// offset and after the last are parts of their own without a group, so that the
-// parts cover all rows. Offsets are clamped to [0, n] and a part that would be
-// negative is empty, so no offsets reach past the matrices. Every lane of a wave
-// makes the calls, with 64 parts looked at per step.
-template <int BM>
-struct GroupTiles {
-  const int32_t* offsets;
-  int n, parts;
-  __device__ __forceinline__ GroupTiles(const LinearArgs& p)
-      : offsets(p.offsets), n((int)p.n), parts(p.groups + 2) {}
-  // The lane's part of a step: rows [*lo, *hi), and its tiles.
-  __device__ __forceinline__ int part(int base, int* lo, int* hi) const {
-    const int i = base + (int)(threadIdx.x % 64);
-    *lo = *hi = 0;
-    if (i < parts) {
-      *lo = i == 0 ? 0 : min(max(offsets[i - 1], 0), n);
-      *hi = i == parts - 1 ? n : min(max(offsets[i], 0), n);
-    }
-    return *hi > *lo ? (int)(((int64_t)(*hi - *lo) + BM - 1) / BM) : 0;
-  }
-  __device__ __forceinline__ int total() const {
-    int sum = 0;
-    for (int base = 0; base < parts; base += 64) {
-      int lo, hi;
-      sum += part(base, &lo, &hi);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return __builtin_amdgcn_readfirstlane(sum);
-  }
-  // Tile `tile` of all parts' tiles but the first SKIP of each.
-  template <int SKIP>
-  __device__ __forceinline__ Rows find(int tile) const {
-    const int lane = threadIdx.x % 64;
-    for (int base = 0; base < parts; base += 64) {
-      int lo, hi;
-      const int tiles = max(part(base, &lo, &hi) - SKIP, 0);
-      int end = tiles;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int up = __shfl_up(end, d);
-        if (lane >= d) end += up;
-      }
-      const uint64_t hit = __ballot(tile < end);
-      if (hit != 0) {
-        const int at = __ffsll((unsigned long long)hit) - 1;
-        const int first = __shfl(end, at) - __shfl(tiles, at), i = base + at;
-        const int row = __shfl(lo, at) + (SKIP + tile - first) * BM;
-        return {__builtin_amdgcn_readfirstlane(row),
-                __builtin_amdgcn_readfirstlane(min(BM, __shfl(hi, at) - row)),
-                __builtin_amdgcn_readfirstlane(i == 0 || i == parts - 1 ? -1 : i - 1)};
-      }
-      tile -= __shfl(end, 63);
-    }
-    return {0, 0, -1};
-  }
-};
-
-// The rows of workgroup y where groups have few: the first BM of part y, found without
-// a search; tiles past a part's first go to the workgroups after the parts'.
-template <int BM, bool GROUPED>
-__device__ __forceinline__ Rows few_rows(const LinearArgs& p) {
-  if constexpr (!GROUPED) {
-    const int64_t row = (int64_t)blockIdx.y * BM;
-    return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
-  } else {
-    const int n = (int)p.n, i = blockIdx.y, last = p.groups + 1;
-    if (i > last) return GroupTiles<BM>(p).template find<1>(i - last - 1);
-    const int lo = i == 0 ? 0 : min(max(p.offsets[i - 1], 0), n);
-    const int hi = i == last ? n : min(max(p.offsets[i], 0), n);
-    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(min(BM, hi - lo)),
-            i == 0 || i == last ? -1 : i - 1};
-  }
-}
-int64_t few_rows_grid(int64_t n, int32_t groups, int64_t bm, bool grouped) {
-  return grouped ? groups + 2 + n / bm : ceil_div64(n, bm);
-}
-
-// Tiles that any offsets cut n rows into, at most.
-int64_t most_slots(int64_t n, int32_t groups, int64_t bm) {
-  return std::min<int64_t>(n, n / bm + groups + 2);
-}
-
 // --- few rows, any alignment: straight from memory ---------------------------------------
 
 // One workgroup: 16 outputs by MT * 16 rows. Its NW waves take the blocks of k in turn, U
@@ -295,13 +205,6 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
 }
 
 // --- tiles through LDS -------------------------------------------------------------
-
-// Workgroup `i` of `total` as the tile that keeps neighbouring tiles on one of the 8
-// XCDs (workgroups go to them in turn), each with its own L2.
-__device__ __forceinline__ uint32_t xcd_tile(uint32_t i, uint32_t total) {
-  const uint32_t q = total / 8, r = total % 8, x = i % 8;
-  return x * q + min(x, r) + i / 8;
-}
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
@@ -429,29 +332,6 @@ struct RowScales {
     return __builtin_amdgcn_raw_buffer_load_b8(res, first + (t * TILE * ld + b), 0, 0);
   }
 };
-
-// The rows and the column tile of this workgroup: bands of group_m row tiles, in each
-// the row tiles of one column tile after another. The grid of a grouped product
-// has room for any offsets; the tiles there are go to the first workgroups, so that all
-// XCDs have as many.
-template <int BM, bool GROUPED>
-__device__ __forceinline__ Rows tile_rows(const LinearArgs& p, uint32_t tiles_n, uint32_t group_m,
-                                          uint32_t* tn) {
-  uint32_t tiles_m = gridDim.x / tiles_n;
-  if constexpr (GROUPED) {
-    tiles_m = (uint32_t)GroupTiles<BM>(p).total();
-    if (blockIdx.x >= tiles_m * tiles_n) return {0, 0, -1};
-  }
-  const uint32_t tile = xcd_tile(blockIdx.x, tiles_m * tiles_n);
-  const uint32_t band = tile / (group_m * tiles_n), in = tile % (group_m * tiles_n);
-  const uint32_t high = min(group_m, tiles_m - band * group_m);
-  // (Divisions are vector code; the buffers built on their results must be scalar.)
-  const uint32_t tm = __builtin_amdgcn_readfirstlane(band * group_m + in % high);
-  *tn = __builtin_amdgcn_readfirstlane(in / high);
-  if constexpr (GROUPED) return GroupTiles<BM>(p).template find<0>((int)tm);
-  const int64_t row = (int64_t)tm * BM;
-  return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
-}
 
 // Writes RUN neighbouring outputs of a row from column n on, of `count` columns. ALL:
 // the caller knows that they are all there.
@@ -991,7 +871,6 @@ TileGrid tile_grid(const LinearArgs& p) {
   const int64_t tiles_n = ceil_div64(p.fout, BN);
   return {tiles_m * tiles_n, tiles_n, std::min<int64_t>(tiles_m, 8)};
 }
-constexpr int64_t kMostTiles = INT32_MAX / 256;
 
 int launched(const char* what) {
   const hipError_t e = hipGetLastError();

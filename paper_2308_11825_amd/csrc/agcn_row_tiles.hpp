@@ -1,0 +1,142 @@
+// The rows of a matrix, or of its groups, cut into tiles, one workgroup each: which rows a
+// workgroup of agcn_qlinear.hip's kernels works on. The groups' offsets are device memory
+// that the caller may fill with anything; whatever they hold, a tile lies inside the matrix.
+//
+// Needs HIP's device functions (hip_runtime.h) or, on the host, stand-ins for them.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+namespace agcn {
+
+// Workgroups of a launch, at most: 2^31 - 1 threads of 256.
+constexpr int64_t kMostTiles = INT32_MAX / 256;
+
+// The rows a tile of at most BM rows works on: rows [row, row + count) of group
+// `group`, or rows of no group (group -1), which are set to 0.
+struct Rows {
+  int64_t row;
+  int32_t count, group;
+};
+
+// The rows cut at the groups' offsets, in tiles of BM. The rows before the first
+// offset and after the last are parts of their own without a group, so that the
+// parts cover all rows. Offsets are clamped to [0, n] and a part that would be
+// negative is empty, so no offsets reach past the matrices. Offsets that decrease make
+// parts that overlap, with any number of tiles in all: sums of tiles end at what is asked
+// of them, so they stay in 32 bits (64 lanes of 2^23 tiles at most, kMostTiles). Every lane
+// of a wave makes the calls, with 64 parts looked at per step.
+template <int BM>
+struct GroupTiles {
+  const int32_t* offsets;
+  int n, parts;
+  template <class Args>  // with the members n, offsets and groups
+  __device__ __forceinline__ explicit GroupTiles(const Args& p)
+      : offsets(p.offsets), n((int)p.n), parts(p.groups + 2) {}
+  // The lane's part of a step: rows [*lo, *hi), and its tiles.
+  __device__ __forceinline__ int part(int base, int* lo, int* hi) const {
+    const int i = base + (int)(threadIdx.x % 64);
+    *lo = *hi = 0;
+    if (i < parts) {
+      *lo = i == 0 ? 0 : min(max(offsets[i - 1], 0), n);
+      *hi = i == parts - 1 ? n : min(max(offsets[i], 0), n);
+    }
+    return *hi > *lo ? (int)(((int64_t)(*hi - *lo) + BM - 1) / BM) : 0;
+  }
+  // The tiles of all parts, or `most` where they are more.
+  __device__ __forceinline__ int total(int most) const {
+    int sum = 0;
+    for (int base = 0; base < parts; base += 64) {
+      int lo, hi;
+      sum += min(part(base, &lo, &hi), most - sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    return __builtin_amdgcn_readfirstlane(min(sum, most));
+  }
+  // Tile `tile` >= 0 of all parts' tiles but the first SKIP of each. (A part's tiles past
+  // that one do not change what is found.)
+  template <int SKIP>
+  __device__ __forceinline__ Rows find(int tile) const {
+    const int lane = threadIdx.x % 64;
+    for (int base = 0; base < parts; base += 64) {
+      int lo, hi;
+      const int tiles = min(max(part(base, &lo, &hi) - SKIP, 0), tile + 1);
+      int end = tiles;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int up = __shfl_up(end, d);
+        if (lane >= d) end += up;
+      }
+      const uint64_t hit = __ballot(tile < end);
+      if (hit != 0) {
+        const int at = __ffsll((unsigned long long)hit) - 1;
+        const int first = __shfl(end, at) - __shfl(tiles, at), i = base + at;
+        const int row = __shfl(lo, at) + (SKIP + tile - first) * BM;
+        return {__builtin_amdgcn_readfirstlane(row),
+                __builtin_amdgcn_readfirstlane(min(BM, __shfl(hi, at) - row)),
+                __builtin_amdgcn_readfirstlane(i == 0 || i == parts - 1 ? -1 : i - 1)};
+      }
+      tile -= __shfl(end, 63);
+    }
+    return {0, 0, -1};
+  }
+};
+
+// The rows of workgroup y where groups have few: the first BM of part y, found without
+// a search; tiles past a part's first go to the workgroups after the parts'.
+template <int BM, bool GROUPED, class Args>
+__device__ __forceinline__ Rows few_rows(const Args& p) {
+  if constexpr (!GROUPED) {
+    const int64_t row = (int64_t)blockIdx.y * BM;
+    return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
+  } else {
+    const int n = (int)p.n, i = blockIdx.y, last = p.groups + 1;
+    if (i > last) return GroupTiles<BM>(p).template find<1>(i - last - 1);
+    const int lo = i == 0 ? 0 : min(max(p.offsets[i - 1], 0), n);
+    const int hi = i == last ? n : min(max(p.offsets[i], 0), n);
+    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(min(BM, hi - lo)),
+            i == 0 || i == last ? -1 : i - 1};
+  }
+}
+inline int64_t few_rows_grid(int64_t n, int32_t groups, int64_t bm, bool grouped) {
+  return grouped ? groups + 2 + n / bm : (n + bm - 1) / bm;
+}
+
+// Tiles that any offsets cut n rows into, at most.
+inline int64_t most_slots(int64_t n, int32_t groups, int64_t bm) {
+  return std::min<int64_t>(n, n / bm + groups + 2);
+}
+
+// Workgroup `i` of `total` as the tile that keeps neighbouring tiles on one of the 8
+// XCDs (workgroups go to them in turn), each with its own L2.
+__device__ __forceinline__ uint32_t xcd_tile(uint32_t i, uint32_t total) {
+  const uint32_t q = total / 8, r = total % 8, x = i % 8;
+  return x * q + min(x, r) + i / 8;
+}
+
+// The rows and the column tile of this workgroup: bands of group_m row tiles, in each
+// the row tiles of one column tile after another. The grid of a grouped product
+// has room for any offsets; the tiles there are go to the first workgroups, so that all
+// XCDs have as many.
+template <int BM, bool GROUPED, class Args>
+__device__ __forceinline__ Rows tile_rows(const Args& p, uint32_t tiles_n, uint32_t group_m,
+                                          uint32_t* tn) {
+  uint32_t tiles_m = gridDim.x / tiles_n;
+  if constexpr (GROUPED) {
+    tiles_m = (uint32_t)GroupTiles<BM>(p).total((int)tiles_m);
+    if (blockIdx.x >= tiles_m * tiles_n) return {0, 0, -1};
+  }
+  const uint32_t tile = xcd_tile(blockIdx.x, tiles_m * tiles_n);
+  const uint32_t band = tile / (group_m * tiles_n), in = tile % (group_m * tiles_n);
+  const uint32_t high = min(group_m, tiles_m - band * group_m);
+  // (Divisions are vector code; the buffers built on their results must be scalar.)
+  const uint32_t tm = __builtin_amdgcn_readfirstlane(band * group_m + in % high);
+  *tn = __builtin_amdgcn_readfirstlane(in / high);
+  if constexpr (GROUPED) return GroupTiles<BM>(p).template find<0>((int)tm);
+  const int64_t row = (int64_t)tm * BM;
+  return {row, (int32_t)min((int64_t)BM, p.n - row), 0};
+}
+
+}  // namespace agcn
