@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "agcn_quant.hpp"
+#include "agcn_row_tiles.hpp"
 
 namespace agcn {
 
@@ -352,7 +353,7 @@ int norm_typed(const NormArgs& a, hipStream_t st) {
 template <class T>
 int quantize_typed(int64_t n, int32_t f, const void* X, int64_t ldx, uint8_t* Q, int64_t ldq,
                    uint8_t* S, int64_t lds, hipStream_t st) {
-  const int64_t blocks = ceil_div64(f, kQBlock), most = std::max<int64_t>(1, (INT32_MAX / 2) / blocks);
+  const int64_t blocks = ceil_div64(f, kQBlock), most = most_quantized_rows(blocks);
   for (int64_t r = 0; r < n; r += most) {
     const int64_t rows = std::min(most, n - r), total = rows * blocks;
     k_quantize_rows<T><<<(unsigned)ceil_div64(total, 16), 256, 0, st>>>(

@@ -13,6 +13,12 @@ namespace agcn {
 // Workgroups of a launch, at most: 2^31 - 1 threads of 256.
 constexpr int64_t kMostTiles = INT32_MAX / 256;
 
+// Rows of `blocks` blocks of 128 columns that one launch quantises, at most: 16 blocks a
+// workgroup of 256 threads.
+constexpr int64_t most_quantized_rows(int64_t blocks) {
+  return std::max<int64_t>(1, kMostTiles * 16 / blocks);
+}
+
 // The rows a tile of at most BM rows works on: rows [row, row + count) of group
 // `group`, or rows of no group (group -1), which are set to 0.
 struct Rows {

@@ -95,9 +95,19 @@ void valid(const Args& p) {
   covers(p, few<BM>(p, -1), 1);
 }
 
+// Launches of the quantiser: fewer than 2^32 threads, and at least a row.
+void quantizer_launches() {
+  for (int64_t blocks : {1, 2, 3, 1000, 131071, 131072}) {
+    const int64_t rows = agcn::most_quantized_rows(blocks);
+    const int64_t threads = (rows * blocks + 15) / 16 * 256;
+    require(rows >= 1 && threads < (int64_t{1} << 32), "a launch too large", Args{rows, nullptr, 0}, blocks, threads);
+  }
+}
+
 }  // namespace
 
 int main() {
+  quantizer_launches();
   std::mt19937 rng(1);
   for (int groups : {0, 1, 5, 62, 63, 130}) {
     for (int n : {1, 64, 500}) {
