@@ -95,6 +95,29 @@ void valid(const Args& p) {
   covers(p, few<BM>(p, -1), 1);
 }
 
+// A workgroup's rows among very many groups take few steps: not one per 64 groups.
+void many_groups() {
+  constexpr int kGroups = 1'000'000;
+  std::vector<int32_t> off(kGroups + 1);
+  for (int rows : {1, 70}) {
+    for (int i = 0; i <= kGroups; ++i) off[(size_t)i] = i * rows;
+    const Args p{(int64_t)kGroups * rows, off.data(), kGroups};
+    const int64_t slots = agcn::most_slots(p.n, kGroups, 64);
+    for (int64_t first : {int64_t{0}, slots / 2, slots - 4}) {
+      const int64_t before = wave::exchanges;
+      const std::vector<Found> found = tiles<64>(p, 1, 4, (uint32_t)first);
+      require(wave::exchanges - before <= 4 * 64 * 40, "steps for four tiles", p, first, wave::exchanges - before);
+      for (const Found& f : found)
+        if (f.rows.count > 0)
+          require(off[(size_t)f.rows.group] <= f.rows.row && f.rows.row + f.rows.count <= off[(size_t)f.rows.group + 1],
+                  "another group's rows", p, f.rows.row, f.rows.group);
+    }
+    const int64_t before = wave::exchanges;
+    few<64>(p, 4, (uint32_t)kGroups + 2);
+    require(wave::exchanges - before <= 4 * 64 * 40, "steps past the first tiles", p, 0, wave::exchanges - before);
+  }
+}
+
 // Launches of the quantiser: fewer than 2^32 threads, and at least a row.
 void quantizer_launches() {
   for (int64_t blocks : {1, 2, 3, 1000, 131071, 131072}) {
@@ -108,9 +131,11 @@ void quantizer_launches() {
 
 int main() {
   quantizer_launches();
+  many_groups();
   std::mt19937 rng(1);
-  for (int groups : {0, 1, 5, 62, 63, 130}) {
-    for (int n : {1, 64, 500}) {
+  for (int groups : {0, 1, 5, 62, 63, 130, 254, 255, 1000, 4000}) {
+    for (int n : {1, 64, 500, 1500}) {
+      if (groups > 200 ? n != (groups == 255 ? 1500 : 64) : n > 500) continue;
       std::vector<int32_t> off((size_t)groups + 1);
       for (int kind = 0; kind < 3; ++kind) {  // spread, most of them empty, all rows in one group
         for (int32_t& o : off)

@@ -27,6 +27,7 @@ inline int64_t held[2][64];  // the values of this exchange and of the one befor
 inline int turn[64];
 inline std::function<void()> body;
 inline int finished;
+inline int64_t exchanges;  // of all lanes
 
 inline void start() {
   body();
@@ -42,6 +43,7 @@ inline void others() {
 template <class T, class F>
 T exchange(T v, F pick) {
   const int t = turn[threadIdx.x] ^= 1;
+  ++exchanges;
   held[t][threadIdx.x] = (int64_t)v;
   others();
   return (T)pick(held[t]);
