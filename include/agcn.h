@@ -329,8 +329,8 @@ int agcn_gcn_layer(agcn_plan_t plan, int32_t fin, int32_t fout, const float* d_X
  * stride and any alignment to the element is taken; rows of Q that start on 16 bytes
  * (pointer and stride) are read fastest. Errors: INVALID_ARGUMENT (negative
  * sizes, strides shorter than a row, NULL pointers with non-empty extents,
- * outputs that overlap inputs or each other, unknown types), UNSUPPORTED (sizes past a
- * launch's limits), HIP. */
+ * outputs that overlap inputs or each other, unknown types), UNSUPPORTED (over 2^24
+ * columns or groups, other sizes past a launch's limits), HIP. */
 
 /* Element types of the 8-bit operators' other matrices. */
 #define AGCN_FLOAT 0  /* 32-bit */

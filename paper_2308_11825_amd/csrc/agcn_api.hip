@@ -851,6 +851,7 @@ int agcn_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtyp
                          int64_t ldw, int64_t group_w, void* d_Q, int64_t ldq, int64_t group_q,
                          void* d_S, int64_t lds, int64_t group_s, void* stream) {
   if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (groups > agcn::kMostWidth) return fail(AGCN_ERR_UNSUPPORTED, "over 2^24 groups");
   if (int rc = check_width(fin, "fin")) return rc;
   if (int rc = check_width(fout, "fout")) return rc;
   int64_t size = 0;
