@@ -514,6 +514,7 @@ def linear(X, W, out=None, stream=None):
 # scales S (torch.float8_e8m0fnu, powers of two), one per 128 columns of a row, or
 # one per 128 x 128 block of a weight. It stands for Q times its scales.
 
+_MOST_INT32 = 2 ** 31 - 1
 _DTYPES = {}  # torch dtype -> AGCN_FLOAT, AGCN_BFLOAT, AGCN_HALF
 _torch = None
 _Q8 = _S8 = None  # the dtypes of values and of scales
@@ -547,7 +548,7 @@ def _matrix(name, t, device, shape, dtype):
     raise ValueError(f"{name} must have shape {tuple(shape)}")
 
 
-def _first(name, t, dims):
+def _first(name, t, dims, weight=False):
     """The shape and device of the tensor that sets a call's sizes and type."""
     if _torch is None:
         _load_torch()
@@ -555,7 +556,11 @@ def _first(name, t, dims):
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dim() != dims:
         raise ValueError(f"{name} must have {dims} dimensions")
-    return t.shape, t.device
+    shape = t.shape
+    # ctypes cuts what the library counts in 32 bits: all sizes but a matrix's rows.
+    if shape[-1] > _MOST_INT32 or (weight and max(shape) > _MOST_INT32):
+        raise ValueError(f"{name} must have at most 2^31 - 1 {'rows, columns and groups' if weight else 'columns'}")
+    return shape, t.device
 
 
 def _dtype_code(name, dtype):
@@ -618,7 +623,7 @@ def quantize_weight(W, stream=None):
     """A weight (fin, fout), as ``linear`` takes it, or one per group (groups, fin,
     fout), in 8 bits for ``quantized_linear`` and ``grouped_linear``: (WQ, WS) with WQ
     (..., fout, fin), transposed, and WS (..., ceil(fout / 128), ceil(fin / 128))."""
-    shape, device = _first("W", W, 3 if getattr(W, "ndim", 2) == 3 else 2)
+    shape, device = _first("W", W, 3 if getattr(W, "ndim", 2) == 3 else 2, weight=True)
     *lead, fin, fout = shape
     dtype = W.dtype
     code, ldw = _dtype_code("W", dtype), _matrix("W", W, device, shape, dtype)
@@ -676,7 +681,7 @@ def rms_norm(X, weight, residual=None, eps=1e-6, hidden=None, out=None, stream=N
 
 def _product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
     shape, device = _first("Q", Q, 2)
-    w_shape, _ = _first("WQ", WQ, 2 if offsets is None else 3)
+    w_shape, _ = _first("WQ", WQ, 2 if offsets is None else 3, weight=True)
     n, fin = shape
     fout = w_shape[-2]
     nb, kb = (fout + 127) // 128, (fin + 127) // 128
