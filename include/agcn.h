@@ -353,7 +353,7 @@ int agcn_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtyp
  * 8 bits in d_Q and d_S, h in d_H. X, R and H are n x f of `dtype`; R may be
  * NULL (h = x), H may be NULL, and H may be X or R itself (same pointer and stride).
  * g: f values of g_dtype, which is dtype or AGCN_FLOAT. Sums and y are
- * in 32 bits from the unrounded h; a row whose squares overflow 32 bits is summed
+ * in 32 bits from the unrounded h; a row whose mean + eps overflows 32 bits is summed
  * scaled. eps > 0 and finite. */
 int agcn_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx,
                   const void* d_R, int64_t ldr, void* d_H, int64_t ldh, const void* d_g,

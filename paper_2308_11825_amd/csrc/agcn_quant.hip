@@ -80,13 +80,11 @@ __device__ __forceinline__ void quantize8(const float (&y)[8], int valid, bool f
   if (first_lane && valid > 0) *s = (uint8_t)code;
 }
 
-// Squares past fp32's range: a row whose sum is not finite is summed again with
-// its values scaled by this, so that only infinities and NaN in it remain.
+// Squares past fp32's range: a row whose mean of squares + eps is not finite is summed again
+// with its values scaled by this, so that only infinities and NaN in it remain.
 constexpr float kTiny = 0x1p-80f;
 
-__device__ __forceinline__ float row_scale(float ss, int32_t f, float eps) {
-  return 1.0f / sqrtf(ss / (float)f + eps);
-}
+__device__ __forceinline__ float mean_eps(float ss, int32_t f, float eps) { return ss / (float)f + eps; }
 
 // Sum over the G lanes (G <= 64) or the workgroup (G = its threads) of a row.
 // `part`: two rows of partial sums, used in turn, so that one barrier a row is
@@ -171,10 +169,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_norm(NormArgs a) {
       }
     }
     ss = row_sum<G>(ss, part, turn);
-    float rs;
-    if (ss <= FLT_MAX) {
-      rs = row_scale(ss, a.f, a.eps);
-    } else {  // the same for every lane of the row
+    float m = mean_eps(ss, a.f, a.eps), rs = 1.0f / sqrtf(m);
+    if (!(m <= FLT_MAX)) {  // the same for every lane of the row
       ss = 0.0f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
@@ -183,7 +179,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_norm(NormArgs a) {
           const float t = h[v][i] * kTiny;
           ss = fmaf(t, t, ss);
         }
-      rs = kTiny * row_scale(row_sum<G>(ss, part + 2, turn), a.f, 0.0f);
+      m = mean_eps(row_sum<G>(ss, part + 2, turn), a.f, a.eps * kTiny * kTiny);
+      rs = kTiny * (1.0f / sqrtf(m));
     }
     uint8_t* q = a.Q + row * a.ldq;
     uint8_t* s = a.S + row * a.lds;
@@ -230,10 +227,11 @@ __global__ __launch_bounds__(1024) void k_rms_norm_long(NormArgs a) {
       }
       return ss;
     };
-    const float ss = row_sum<G>(squares(1.0f), part, turn);
-    const float rs = ss <= FLT_MAX
-                         ? row_scale(ss, a.f, a.eps)
-                         : kTiny * row_scale(row_sum<G>(squares(kTiny), part + 2, turn), a.f, 0.0f);
+    float m = mean_eps(row_sum<G>(squares(1.0f), part, turn), a.f, a.eps), rs = 1.0f / sqrtf(m);
+    if (!(m <= FLT_MAX)) {
+      m = mean_eps(row_sum<G>(squares(kTiny), part + 2, turn), a.f, a.eps * kTiny * kTiny);
+      rs = kTiny * (1.0f / sqrtf(m));
+    }
     uint8_t* q = a.Q + row * a.ldq;
     uint8_t* s = a.S + row * a.lds;
     for (int64_t c0 = 0; c0 < a.f; c0 += G * 8) {  // whole waves: the blocks' DPP steps
