@@ -362,11 +362,14 @@ int agcn_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t 
 
 /* Y = epilogue(A W^T), n x fout of `dtype`: A n rows of fin in 8 bits (d_Q,
  * d_S), W fout rows of fin in 8 bits (d_WQ, d_WS). Sums are in 32 bits. For
- * AGCN_FLOAT and AGCN_HALF the products are exact and the error that of fp32 sums. For
- * AGCN_BFLOAT the 8-bit matrix instruction adds them: of each eight neighbouring products
- * what lies more than 13 bits below the largest is cut off (1.5e-5 of the result's
- * 2-norm for normal values, a hundredth of the rounding to the type; at most 7 * 2^-13 of the
- * sum of the eights' largest). fin = 0 gives Y = 0. */
+ * AGCN_FLOAT and AGCN_HALF the products are exact and the error that of fp32 sums (8e-8 of
+ * the result's 2-norm at fin = 4096), where values times their scales fit bfloat16: what lies
+ * below 2^-133 in a block with one of the three least scales is cut off, and 2^128 and
+ * above is infinite, whatever the other factor. For AGCN_BFLOAT the 8-bit matrix
+ * instruction multiplies: of each eight neighbouring products what lies more than 13 bits
+ * below the largest is cut off, at most 7 * 2^-13 of the sum of the eights' largest. For normal
+ * values, or ones of one sign, that is 1.5e-5 of the result's 2-norm at any fin, a hundredth
+ * of the rounding to the type. fin = 0 gives Y = 0. */
 int agcn_quantized_linear(int64_t n, int32_t fin, int32_t fout, const void* d_Q, int64_t ldq,
                           const void* d_S, int64_t lds, const void* d_WQ, int64_t ldwq,
                           const void* d_WS, int64_t ldws, int32_t dtype, void* d_Y, int64_t ldy,
