@@ -8,9 +8,12 @@
 // k_rms_norm: h = x + r, y = h / sqrt(mean(h^2) + eps) * g, then y's blocks.
 // k_quantize_rows: the blocks of x itself. k_quantize_weight: those of W^T.
 //
-// All are bound by memory: each value is read once and held in registers from
-// the sum of squares to the 8 bits, and 16 lanes of 8 values make one block, so
-// a block's largest value needs four DPP steps and no LDS.
+// All have little to do but read and write: each value is read once and held in registers
+// from the sum of squares to the 8 bits, and 16 lanes of 8 values make one block, so
+// a block's largest value needs four DPP steps and no LDS. Rows of one vector a lane are bound
+// by memory. 16-bit rows of several are not yet: the compiler waits for a vector's
+// values before it asks for the next one's, as they are converted where they are loaded
+// (60,000 x 601 float16 26 us, 4.2 TB/s), and so for the 64 values of k_quantize_weight.
 #include <algorithm>
 
 #include "agcn_quant.hpp"
