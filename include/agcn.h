@@ -22,7 +22,11 @@
  * cores, no plan needed) and agcn_gcn_layer (linear, then the aggregation
  * with the activation). For inference in 8 bits: agcn_rms_norm,
  * agcn_quantize_rows, agcn_quantize_weight, agcn_quantized_linear and
- * agcn_grouped_linear, no plan needed either.
+ * agcn_grouped_linear, no plan needed either; the same with 8-bit integers:
+ * agcn_quantize_rows_int, agcn_quantize_weight_int, agcn_int_linear and
+ * agcn_grouped_int_linear. For layers whose rows go to a few of many weights:
+ * agcn_layer_norm, agcn_sort_groups, agcn_dispatch and agcn_combine, with
+ * gradients.
  *
  * Conventions for every call:
  *   - Pointers named d_* are device pointers (memory of the current HIP
@@ -387,6 +391,125 @@ int agcn_grouped_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, co
                         int64_t group_wq, const void* d_WS, int64_t ldws, int64_t group_ws,
                         const int32_t* d_offsets, int32_t dtype, void* d_Y, int64_t ldy,
                         void* stream, int32_t epilogue);
+
+/* ---- products of 8-bit integers -----------------------------------------
+ *
+ * A matrix in 8-bit integers is Q, values of -128 to 127, one byte each,
+ * row-major, and S, one float per row (contiguous; for a weight per output, which
+ * is a row of its transposed values), and stands for S[row] * Q. With a the largest
+ * |x| of a row, the quantisers give q = x * (127 / a), the quotient and the product
+ * rounded to 32 bits, rounded to nearest even, and S = a / 127. A row
+ * of zeros has S = 0; one that holds an infinity or NaN has S = NaN, and so
+ * has every result of it.
+ *
+ * Asynchronous on `stream`, without workspace or allocation, so they can be
+ * captured into a graph; results do not depend on timing. Strides, alignment
+ * and errors as for the 8-bit operators above. */
+
+/* The rows of X (n x f, dtype) in 8-bit integers: d_Q n x f, d_S n floats. */
+int agcn_quantize_rows_int(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, void* d_Q,
+                           int64_t ldq, float* d_S, void* stream);
+
+/* Weights W (groups x fin x fout, as agcn_quantize_weight takes them) in 8-bit
+ * integers, transposed: d_Q holds fout rows of fin values per group, d_S fout
+ * floats, group_s floats from one group to the next. */
+int agcn_quantize_weight_int(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* d_W,
+                             int64_t ldw, int64_t group_w, void* d_Q, int64_t ldq, int64_t group_q,
+                             float* d_S, int64_t group_s, void* stream);
+
+/* Y = epilogue(A W^T), n x fout of `dtype`: A n rows of fin (d_Q, d_S), W fout
+ * rows of fin (d_WQ, d_WS). Y[m][n] = (sum * d_S[m]) * d_WS[n] with the exact sum of
+ * the integers' products, rounded to 32 bits before and after each product with a
+ * scale. fin = 0 gives Y = 0. UNSUPPORTED for fin of 2^17 and over, whose sums can leave
+ * 32 bits. */
+int agcn_int_linear(int64_t n, int32_t fin, int32_t fout, const void* d_Q, int64_t ldq, const float* d_S,
+                    const void* d_WQ, int64_t ldwq, const float* d_WS, int32_t dtype, void* d_Y,
+                    int64_t ldy, void* stream, int32_t epilogue);
+
+/* The same with a weight per group of rows: d_offsets, groups, empty groups and
+ * rows of no group as in agcn_grouped_linear. */
+int agcn_grouped_int_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q,
+                            int64_t ldq, const float* d_S, const void* d_WQ, int64_t ldwq,
+                            int64_t group_wq, const float* d_WS, int64_t group_ws,
+                            const int32_t* d_offsets, int32_t dtype, void* d_Y, int64_t ldy,
+                            void* stream, int32_t epilogue);
+
+/* ---- layer norm ---------------------------------------------------------
+ *
+ * Asynchronous on `stream`, no allocation; sums do not depend on timing (no
+ * atomics). Matrices are n x f of `dtype` with any stride and any alignment to the
+ * element; parameters are f values of p_dtype, which is dtype or AGCN_FLOAT.
+ * Errors as for the 8-bit operators. */
+
+/* h = x + r, y = (h - mean) / sqrt(var + eps) * g + b per row: mean and var (of
+ * the f values, not f - 1) are of the unrounded h, in 32 bits, and a row whose sums
+ * overflow them is summed scaled. d_R may be NULL (h = x); d_H, where h is written, may be
+ * NULL, or X or R itself (same pointer and stride); d_b may be NULL. d_stats, unless
+ * NULL: n rows of mean and 1 / sqrt(var + eps), two floats at stride lds >= 2, as
+ * agcn_layer_norm_backward takes them. A row that holds an infinity or NaN is NaN. eps > 0
+ * and finite. */
+int agcn_layer_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, const void* d_R,
+                    int64_t ldr, void* d_H, int64_t ldh, const void* d_g, const void* d_b,
+                    int32_t p_dtype, float eps, void* d_Y, int64_t ldy, float* d_stats, int64_t lds,
+                    void* stream);
+
+/* Bytes of workspace of agcn_layer_norm_backward for the sums of dg and db. */
+int agcn_layer_norm_workspace_size(int64_t n, int32_t f, int32_t dtype, size_t* bytes);
+
+/* Gradients of agcn_layer_norm from dY, that of y: with xh = (h - mean) / sqrt(var +
+ * eps) and d = dy * g, per row dx = (d - mean(d) - xh * mean(d * xh)) / sqrt(var + eps) +
+ * dh (the gradient of x and of r), and over the rows dg = sum of dy * xh, db = sum of
+ * dy. d_H: the rows h (X without a residual); d_dH: the gradient of h from elsewhere, or
+ * NULL; d_dg, d_db: f values of p_dtype each, or NULL (not wanted). d_ws:
+ * agcn_layer_norm_workspace_size bytes, 4-byte aligned; may be NULL when dg and db both are. */
+int agcn_layer_norm_backward(int64_t n, int32_t f, int32_t dtype, const void* d_dY, int64_t lddy,
+                             const void* d_H, int64_t ldh, const void* d_dH, int64_t lddh,
+                             const float* d_stats, int64_t lds, const void* d_g, int32_t p_dtype,
+                             void* d_dX, int64_t lddx, void* d_dg, void* d_db, void* d_ws,
+                             void* stream);
+
+/* ---- rows sent to groups and back ---------------------------------------
+ *
+ * Each of n rows goes to k groups (experts, types), as in a routed layer: sort,
+ * lay the rows out in group order, multiply them by their groups' weights
+ * (agcn_grouped_linear, agcn_grouped_int_linear), and add them up per row. n * k is at most
+ * 2^31 - 1. Asynchronous on `stream`, no allocation; results do not depend on timing.
+ * Errors as for the 8-bit operators. */
+
+/* Bytes of workspace of agcn_sort_groups (0 for few ids and groups). */
+int agcn_sort_groups_workspace_size(int64_t n, int32_t k, int32_t groups, size_t* bytes);
+
+/* Sorts the n * k ids (d_ids, n rows of k integers of id_bytes 4 or 8, stride ldi) by
+ * group, keeping the order of ids of a group. d_place (n x k, stride ldp): where each goes,
+ * 0 to n * k - 1. d_offsets: groups + 1 integers, group e has the places d_offsets[e] to
+ * d_offsets[e + 1] - 1. Ids outside [0, groups) have no group: they get the places from
+ * d_offsets[groups] on, and place p is written as -1 - p. d_ws:
+ * agcn_sort_groups_workspace_size bytes, 4-byte aligned. UNSUPPORTED over 65536 groups. */
+int agcn_sort_groups(int64_t n, int32_t k, int32_t groups, const void* d_ids, int32_t id_bytes,
+                     int64_t ldi, int32_t* d_offsets, int32_t* d_place, int64_t ldp, void* d_ws,
+                     void* stream);
+
+/* Y[place[t][c]] = X[t], rows of `bytes` bytes of any type (strides in bytes too): Y has n * k
+ * rows, and those of ids without a group are set to 0. Its gradient is agcn_combine without
+ * weights. Places that are not agcn_sort_groups' leave rows unwritten or written more than
+ * once; none reaches past the matrices, here and below. */
+int agcn_dispatch(int64_t n, int32_t k, int64_t bytes, const void* d_X, int64_t ldx,
+                  const int32_t* d_place, int64_t ldp, void* d_Y, int64_t ldy, void* stream);
+
+/* Y[t] = sum over c of W[t][c] * R[place[t][c]], added in 32 bits in the order of c: R n * k
+ * rows and Y n rows of f values of `dtype`, W n x k floats or NULL (all 1). Ids without a
+ * group are left out, whatever their weight and row hold. */
+int agcn_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* d_R, int64_t ldr,
+                 const int32_t* d_place, int64_t ldp, const float* d_W, int64_t ldw, void* d_Y,
+                 int64_t ldy, void* stream);
+
+/* Gradients of agcn_combine from dY, that of Y: dR[place[t][c]] = W[t][c] * dY[t] and dW[t][c]
+ * = sum over the columns of dY[t] * R[place[t][c]], in 32 bits; both are 0 for ids without a
+ * group. (Without weights dR is agcn_dispatch of dY.) */
+int agcn_combine_backward(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* d_dY,
+                          int64_t lddy, const void* d_R, int64_t ldr, const int32_t* d_place,
+                          int64_t ldp, const float* d_W, int64_t ldw, void* d_dR, int64_t lddr,
+                          float* d_dW, int64_t lddw, void* stream);
 
 /* Fills *out. Host-only, no HIP call. */
 int agcn_plan_info(agcn_plan_t plan, agcn_plan_stats* out);

@@ -21,8 +21,13 @@ __all__ = [
     "agcn_release_cached_memory", "agcn_spmm_ex", "agcn_linear", "agcn_gcn_workspace_size",
     "agcn_gcn_layer", "agcn_spmm_noalloc", "AGCN_NOALLOC_MAX_WORKSPACE", "agcn_quantize_rows",
     "agcn_quantize_weight", "agcn_rms_norm", "agcn_quantized_linear", "agcn_grouped_linear",
-    "Plan", "linear", "quantize", "quantize_weight", "rms_norm", "quantized_linear",
-    "grouped_linear", "PlanParams", "PlanStats", "EXPORTED_SYMBOLS",
+    "agcn_quantize_rows_int", "agcn_quantize_weight_int", "agcn_int_linear",
+    "agcn_grouped_int_linear", "agcn_layer_norm", "agcn_layer_norm_workspace_size",
+    "agcn_layer_norm_backward", "agcn_sort_groups_workspace_size", "agcn_sort_groups",
+    "agcn_dispatch", "agcn_combine", "agcn_combine_backward", "Plan", "linear", "quantize", "quantize_weight", "rms_norm", "quantized_linear",
+    "grouped_linear", "quantize_int", "quantize_weight_int", "int_linear", "grouped_int_linear",
+    "layer_norm", "layer_norm_backward", "sort_groups", "dispatch", "combine", "combine_backward",
+    "PlanParams", "PlanStats", "EXPORTED_SYMBOLS",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -34,7 +39,10 @@ EXPORTED_SYMBOLS = [
     "agcn_status_string", "agcn_last_error", "agcn_release_cached_memory", "agcn_spmm_ex",
     "agcn_linear", "agcn_gcn_workspace_size", "agcn_gcn_layer", "agcn_spmm_noalloc",
     "agcn_quantize_rows", "agcn_quantize_weight", "agcn_rms_norm", "agcn_quantized_linear",
-    "agcn_grouped_linear",
+    "agcn_grouped_linear", "agcn_quantize_rows_int", "agcn_quantize_weight_int", "agcn_int_linear",
+    "agcn_grouped_int_linear", "agcn_layer_norm", "agcn_layer_norm_workspace_size",
+    "agcn_layer_norm_backward", "agcn_sort_groups_workspace_size", "agcn_sort_groups",
+    "agcn_dispatch", "agcn_combine", "agcn_combine_backward",
 ]
 
 AGCN_OK = 0
@@ -165,6 +173,26 @@ def load_library(path: str | None = None):
     lib.agcn_grouped_linear.argtypes = [i64, i32, i32, i32, _vp, i64, _vp, i64, _vp, i64, i64, _vp,
                                         i64, i64, _vp, i32, _vp, i64, _vp, i32]
     lib.agcn_grouped_linear.restype = ctypes.c_int
+    lib.agcn_quantize_rows_int.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, _vp]
+    lib.agcn_quantize_weight_int.argtypes = [i32, i32, i32, i32, _vp, i64, i64, _vp, i64, i64, _vp,
+                                             i64, _vp]
+    lib.agcn_int_linear.argtypes = [i64, i32, i32, _vp, i64, _vp, _vp, i64, _vp, i32, _vp, i64, _vp,
+                                    i32]
+    lib.agcn_grouped_int_linear.argtypes = [i64, i32, i32, i32, _vp, i64, _vp, _vp, i64, i64, _vp,
+                                            i64, _vp, i32, _vp, i64, _vp, i32]
+    lib.agcn_layer_norm.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, _vp, i32,
+                                    ctypes.c_float, _vp, i64, _vp, i64, _vp]
+    lib.agcn_layer_norm_workspace_size.argtypes = [i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.agcn_layer_norm_backward.argtypes = [i64, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i64,
+                                             _vp, i32, _vp, i64, _vp, _vp, _vp, _vp]
+    lib.agcn_sort_groups_workspace_size.argtypes = [i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.agcn_sort_groups.argtypes = [i64, i32, i32, _vp, i32, i64, _vp, _vp, i64, _vp, _vp]
+    lib.agcn_dispatch.argtypes = [i64, i32, i64, _vp, i64, _vp, i64, _vp, i64, _vp]
+    lib.agcn_combine.argtypes = [i64, i32, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i64, _vp]
+    lib.agcn_combine_backward.argtypes = [i64, i32, i32, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i64,
+                                          _vp, i64, _vp, i64, _vp]
+    for name in EXPORTED_SYMBOLS[EXPORTED_SYMBOLS.index("agcn_quantize_rows_int"):]:
+        getattr(lib, name).restype = ctypes.c_int
     lib.agcn_plan_info.argtypes = [_vp, ctypes.POINTER(PlanStats)]
     lib.agcn_plan_info.restype = ctypes.c_int
     lib.agcn_plan_export.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp]
@@ -270,6 +298,74 @@ def agcn_grouped_linear(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq, gr
     _check(load_library().agcn_grouped_linear(n, fin, fout, groups, d_Q, ldq, d_S, lds, d_WQ, ldwq,
                                               group_wq, d_WS, ldws, group_ws, d_offsets, dtype, d_Y,
                                               ldy, stream, epilogue))
+
+
+def agcn_quantize_rows_int(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, stream=0):
+    _check(load_library().agcn_quantize_rows_int(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, stream))
+
+
+def agcn_quantize_weight_int(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q, ldq, group_q, d_S,
+                             group_s, stream=0):
+    _check(load_library().agcn_quantize_weight_int(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q,
+                                                   ldq, group_q, d_S, group_s, stream))
+
+
+def agcn_int_linear(n, fin, fout, d_Q, ldq, d_S, d_WQ, ldwq, d_WS, dtype, d_Y, ldy, stream=0,
+                    epilogue=AGCN_EPILOGUE_NONE):
+    _check(load_library().agcn_int_linear(n, fin, fout, d_Q, ldq, d_S, d_WQ, ldwq, d_WS, dtype, d_Y,
+                                          ldy, stream, epilogue))
+
+
+def agcn_grouped_int_linear(n, fin, fout, groups, d_Q, ldq, d_S, d_WQ, ldwq, group_wq, d_WS, group_ws,
+                            d_offsets, dtype, d_Y, ldy, stream=0, epilogue=AGCN_EPILOGUE_NONE):
+    _check(load_library().agcn_grouped_int_linear(n, fin, fout, groups, d_Q, ldq, d_S, d_WQ, ldwq,
+                                                  group_wq, d_WS, group_ws, d_offsets, dtype, d_Y,
+                                                  ldy, stream, epilogue))
+
+
+def agcn_layer_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, d_b, p_dtype, eps, d_Y, ldy,
+                    d_stats, lds, stream=0):
+    _check(load_library().agcn_layer_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, d_b,
+                                          p_dtype, eps, d_Y, ldy, d_stats, lds, stream))
+
+
+def agcn_layer_norm_workspace_size(n, f, dtype) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().agcn_layer_norm_workspace_size(n, f, dtype, ctypes.byref(b)))
+    return b.value
+
+
+def agcn_layer_norm_backward(n, f, dtype, d_dY, lddy, d_H, ldh, d_dH, lddh, d_stats, lds, d_g,
+                             p_dtype, d_dX, lddx, d_dg, d_db, d_ws, stream=0):
+    _check(load_library().agcn_layer_norm_backward(n, f, dtype, d_dY, lddy, d_H, ldh, d_dH, lddh,
+                                                   d_stats, lds, d_g, p_dtype, d_dX, lddx, d_dg,
+                                                   d_db, d_ws, stream))
+
+
+def agcn_sort_groups_workspace_size(n, k, groups) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().agcn_sort_groups_workspace_size(n, k, groups, ctypes.byref(b)))
+    return b.value
+
+
+def agcn_sort_groups(n, k, groups, d_ids, id_bytes, ldi, d_offsets, d_place, ldp, d_ws, stream=0):
+    _check(load_library().agcn_sort_groups(n, k, groups, d_ids, id_bytes, ldi, d_offsets, d_place,
+                                           ldp, d_ws, stream))
+
+
+def agcn_dispatch(n, k, nbytes, d_X, ldx, d_place, ldp, d_Y, ldy, stream=0):
+    _check(load_library().agcn_dispatch(n, k, nbytes, d_X, ldx, d_place, ldp, d_Y, ldy, stream))
+
+
+def agcn_combine(n, k, f, dtype, d_R, ldr, d_place, ldp, d_W, ldw, d_Y, ldy, stream=0):
+    _check(load_library().agcn_combine(n, k, f, dtype, d_R, ldr, d_place, ldp, d_W, ldw, d_Y, ldy,
+                                       stream))
+
+
+def agcn_combine_backward(n, k, f, dtype, d_dY, lddy, d_R, ldr, d_place, ldp, d_W, ldw, d_dR, lddr,
+                          d_dW, lddw, stream=0):
+    _check(load_library().agcn_combine_backward(n, k, f, dtype, d_dY, lddy, d_R, ldr, d_place, ldp,
+                                                d_W, ldw, d_dR, lddr, d_dW, lddw, stream))
 
 
 def agcn_plan_info(plan) -> PlanStats:
@@ -589,14 +685,14 @@ def _new(like, stream, shape, dtype):
         return like.new_empty(shape, dtype=dtype)
 
 
-def _new_rows(like, stream, lead, k):
-    """Values (..., k) in 8 bits and their row stride: rows start on 16 bytes, on 128 (the
+def _new_rows(like, stream, lead, k, dtype=None):
+    """Values (..., k) in 8 bits (e4m3 unless told otherwise) and their row stride: rows start on 16 bytes, on 128 (the
     lines of memory, which a block of 128 columns then is one of) where that adds an
     eighth at most: 230,000 x 602 -> 256 bfloat16 78 us with rows of 640 bytes, 83 with 608."""
     ld = (k + 127) // 128 * 128
     if ld > k + k // 8:
         ld = (k + 15) // 16 * 16
-    q = _new(like, stream, (*lead, ld), _Q8)
+    q = _new(like, stream, (*lead, ld), _Q8 if dtype is None else dtype)
     return (q[..., :k] if k != ld else q), ld
 
 
@@ -732,3 +828,302 @@ def grouped_linear(Q, S, WQ, WS, offsets, dtype=None, act=None, out=None, stream
     if not hasattr(offsets, "data_ptr"):
         raise TypeError("offsets must be an int32 CUDA tensor")
     return _product(Q, S, WQ, WS, offsets, dtype, act, out, stream)
+
+
+# ---- products of 8-bit integers ----
+#
+# A matrix in 8-bit integers is a pair of tensors: the values Q (torch.int8) and a float32
+# scale S for each row, or for each output of a weight. It stands for Q times its scales.
+
+def _vector(name, t, device, shape, dtype):
+    """Checks `t`, a contiguous vector (or stacked ones, contiguous each) of this shape."""
+    if not isinstance(t, _torch.Tensor) or t.device != device:
+        raise TypeError(f"{name} must be a tensor on {device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous")
+
+
+def quantize_int(X, out=None, stream=None):
+    """The rows of X (n, f) in 8-bit integers: (Q, S), Q (n, f) int8 and S (n,) float32, a
+    127th of the row's largest value. X: float32, bfloat16 or float16 CUDA tensor; out: such a
+    pair to write to."""
+    (n, f), device = _first("X", X, 2)
+    dtype = X.dtype
+    code, ldx = _dtype_code("X", dtype), _matrix("X", X, device, X.shape, dtype)
+    if out is None:
+        Q, ldq = _new_rows(X, stream, (n,), f, _torch.int8)
+        S = _new(X, stream, (n,), _torch.float32)
+    else:
+        Q, S = out
+        ldq = _matrix("out[0]", Q, device, (n, f), _torch.int8)
+        _vector("out[1]", S, device, (n,), _torch.float32)
+    st = _on_stream(device, stream, (X, Q, S))
+    _call(device, agcn_quantize_rows_int, n, f, code, X.data_ptr(), ldx, Q.data_ptr(), ldq,
+          S.data_ptr(), st)
+    return Q, S
+
+
+def quantize_weight_int(W, stream=None):
+    """A weight (fin, fout), as ``linear`` takes it, or one per group (groups, fin, fout), in
+    8-bit integers for ``int_linear`` and ``grouped_int_linear``: (WQ, WS) with WQ (..., fout,
+    fin), transposed, and WS (..., fout) float32."""
+    shape, device = _first("W", W, 3 if getattr(W, "ndim", 2) == 3 else 2, weight=True)
+    *lead, fin, fout = shape
+    dtype = W.dtype
+    code, ldw = _dtype_code("W", dtype), _matrix("W", W, device, shape, dtype)
+    Q, ldq = _new_rows(W, stream, (*lead, fout), fin, _torch.int8)
+    S = _new(W, stream, (*lead, fout), _torch.float32)
+    st = _on_stream(device, stream, (W,))
+    groups, strides = (lead[0], [t.stride(0) for t in (W, Q, S)]) if lead else (1, (0, 0, 0))
+    _call(device, agcn_quantize_weight_int, groups, fin, fout, code, W.data_ptr(), ldw, strides[0],
+          Q.data_ptr(), ldq, strides[1], S.data_ptr(), strides[2], st)
+    return Q, S
+
+
+def _int_product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
+    shape, device = _first("Q", Q, 2)
+    w_shape, _ = _first("WQ", WQ, 2 if offsets is None else 3, weight=True)
+    n, fin = shape
+    fout, lead = w_shape[-2], w_shape[:-2]
+    ldq = _matrix("Q", Q, device, shape, _torch.int8)
+    _vector("S", S, device, (n,), _torch.float32)
+    ldwq = _matrix("WQ", WQ, device, (*lead, fout, fin), _torch.int8)
+    _vector("WS", WS, device, (*lead, fout), _torch.float32)
+    epilogue = _EPILOGUES.get(act)
+    if epilogue is None:
+        raise ValueError("act must be None, 'none' or 'relu'")
+    if out is None:
+        dtype = _torch.float32 if dtype is None else dtype
+        code = _dtype_code("the result", dtype)
+        out, ldy = _new(Q, stream, (n, fout), dtype), fout
+    else:
+        code = _dtype_code("out", getattr(out, "dtype", None))
+        ldy = _matrix("out", out, device, (n, fout), out.dtype if dtype is None else dtype)
+    st = _on_stream(device, stream, (Q, S, WQ, WS, offsets, out))
+    if offsets is None:
+        _call(device, agcn_int_linear, n, fin, fout, Q.data_ptr(), ldq, S.data_ptr(), WQ.data_ptr(),
+              ldwq, WS.data_ptr(), code, out.data_ptr(), ldy, st, epilogue)
+        return out
+    groups = lead[0]
+    _vector("offsets", offsets, device, (groups + 1,), _torch.int32)
+    _call(device, agcn_grouped_int_linear, n, fin, fout, groups, Q.data_ptr(), ldq, S.data_ptr(),
+          WQ.data_ptr(), ldwq, WQ.stride(0), WS.data_ptr(), WS.stride(0), offsets.data_ptr(), code,
+          out.data_ptr(), ldy, st, epilogue)
+    return out
+
+
+def int_linear(Q, S, WQ, WS, dtype=None, act=None, out=None, stream=None):
+    """act(A W^T), (n, fout), of A (n, fin) and W (fout, fin) in 8-bit integers, as
+    ``quantize_int`` and ``quantize_weight_int`` give them. dtype: float32 (the default),
+    bfloat16 or float16; the integers' sums are exact, fin below 2^17; act: None or "relu"."""
+    return _int_product(Q, S, WQ, WS, None, dtype, act, out, stream)
+
+
+def grouped_int_linear(Q, S, WQ, WS, offsets, dtype=None, act=None, out=None, stream=None):
+    """``int_linear`` with a weight per group of rows, as ``grouped_linear``: rows offsets[e]
+    to offsets[e + 1] - 1 take WQ[e], WS[e]; rows of no group are 0."""
+    if not hasattr(offsets, "data_ptr"):
+        raise TypeError("offsets must be an int32 CUDA tensor")
+    return _int_product(Q, S, WQ, WS, offsets, dtype, act, out, stream)
+
+
+# ---- layer norm ----
+
+def layer_norm(X, weight, bias=None, residual=None, eps=1e-5, stats=False, hidden=None, out=None,
+               stream=None):
+    """y = (h - mean) / sqrt(var + eps) * weight + bias per row of h = X + residual: y; with a
+    residual (y, h); with stats=True one more, (n, 2) float32, each row's mean and
+    1 / sqrt(var + eps) for ``layer_norm_backward`` (no gradient is recorded).
+
+    X, residual, h and y are (n, f) of one type (float32, bfloat16 or float16), weight and bias
+    (f,) both of that type or float32. hidden: where h is written (X or residual itself will
+    do); out: where y is."""
+    (n, f), device = _first("X", X, 2)
+    dtype, shape = X.dtype, X.shape
+    code, ldx = _dtype_code("X", dtype), _matrix("X", X, device, shape, dtype)
+    p_code = _parameter("weight", weight, device, f, dtype)
+    b = None
+    if bias is not None:
+        _vector("bias", bias, device, (f,), weight.dtype)
+        b = bias.data_ptr()
+    r = h = s = None
+    ldr = ldh = 0
+    if residual is not None:
+        ldr = _matrix("residual", residual, device, shape, dtype)
+        r = residual.data_ptr()
+        if hidden is None:
+            hidden, ldh = _new(X, stream, shape, dtype), f
+        else:
+            ldh = _matrix("hidden", hidden, device, shape, dtype)
+        h = hidden.data_ptr()
+    elif hidden is not None:
+        raise ValueError("hidden needs a residual: without one h is X")
+    if out is None:
+        out, ldy = _new(X, stream, shape, dtype), f
+    else:
+        ldy = _matrix("out", out, device, shape, dtype)
+    if stats:
+        if f == 0:
+            raise ValueError("rows of no columns have no statistics")
+        stats = _new(X, stream, (n, 2), _torch.float32)
+        s = stats.data_ptr()
+    st = _on_stream(device, stream, (X, weight, bias, residual, hidden, out))
+    _call(device, agcn_layer_norm, n, f, code, X.data_ptr(), ldx, r, ldr, h, ldh, weight.data_ptr(),
+          b, p_code, eps, out.data_ptr(), ldy, s, 2, st)
+    results = (out,) if residual is None else (out, hidden)
+    if stats is not False:
+        results += (stats,)
+    return results if len(results) > 1 else out
+
+
+def _parameter(name, t, device, f, dtype):
+    """The type code of a norm's parameter, (f,) float32 or of the rows' type."""
+    if not isinstance(t, _torch.Tensor) or t.device != device:
+        raise TypeError(f"{name} must be a tensor on X's device")
+    if t.dtype is not dtype and t.dtype is not _torch.float32:
+        raise TypeError(f"{name} must be float32 or of X's type")
+    _vector(name, t, device, (f,), t.dtype)
+    return _DTYPES[t.dtype]
+
+
+def layer_norm_backward(grad, H, stats, weight, bias=True, grad_hidden=None, out=None, stream=None):
+    """Gradients of ``layer_norm`` from grad, that of y: (dX, dweight, dbias). H: the rows h (X
+    where there was no residual); stats: as ``layer_norm`` gave them; grad_hidden: the gradient
+    of h from elsewhere, added to dX, which is that of X and of the residual; bias=False: dbias
+    is None; out: where dX is written. dweight and dbias have weight's type."""
+    (n, f), device = _first("grad", grad, 2)
+    dtype, shape = grad.dtype, grad.shape
+    code, lddy = _dtype_code("grad", dtype), _matrix("grad", grad, device, shape, dtype)
+    ldh = _matrix("H", H, device, shape, dtype)
+    lds = _matrix("stats", stats, device, (n, 2), _torch.float32)
+    p_code = _parameter("weight", weight, device, f, dtype)
+    d = None
+    ldd = 0
+    if grad_hidden is not None:
+        ldd = _matrix("grad_hidden", grad_hidden, device, shape, dtype)
+        d = grad_hidden.data_ptr()
+    if out is None:
+        out, lddx = _new(grad, stream, shape, dtype), f
+    else:
+        lddx = _matrix("out", out, device, shape, dtype)
+    dw = _new(grad, stream, (f,), weight.dtype)
+    db = _new(grad, stream, (f,), weight.dtype) if bias else None
+    nb = agcn_layer_norm_workspace_size(n, f, code)
+    ws = _new(grad, stream, (nb // 4,), _torch.float32) if nb else None
+    st = _on_stream(device, stream, (grad, H, stats, weight, grad_hidden, out))
+    _call(device, agcn_layer_norm_backward, n, f, code, grad.data_ptr(), lddy, H.data_ptr(), ldh, d,
+          ldd, stats.data_ptr(), lds, weight.data_ptr(), p_code, out.data_ptr(), lddx, dw.data_ptr(),
+          db.data_ptr() if bias else None, ws.data_ptr() if nb else None, st)
+    return out, dw, db
+
+
+# ---- rows sent to groups and back ----
+
+def sort_groups(ids, groups, out=None, stream=None):
+    """Sorts ids (n, k), each row's group ids (int32 or int64 CUDA tensor), by group: (offsets,
+    place), int32. place (n, k): where each id goes, in the order of the groups and within a
+    group of the ids; offsets (groups + 1,): group e has the places offsets[e] to
+    offsets[e + 1] - 1, as ``grouped_linear`` takes them. Ids outside [0, groups) get the
+    places from offsets[groups] on, written as -1 - place. out: such a pair to write to."""
+    (n, k), device = _first("ids", ids, 2)
+    if ids.dtype is not _torch.int32 and ids.dtype is not _torch.int64:
+        raise TypeError("ids must have dtype int32 or int64")
+    if not 0 <= groups <= _MOST_INT32:
+        raise ValueError("groups must be from 0 to 2^31 - 1")
+    groups = int(groups)
+    ldi = _matrix("ids", ids, device, (n, k), ids.dtype)
+    if out is None:
+        offsets = _new(ids, stream, (groups + 1,), _torch.int32)
+        place, ldp = _new(ids, stream, (n, k), _torch.int32), k
+    else:
+        offsets, place = out
+        _vector("out[0]", offsets, device, (groups + 1,), _torch.int32)
+        ldp = _matrix("out[1]", place, device, (n, k), _torch.int32)
+    nb = agcn_sort_groups_workspace_size(n, k, groups)
+    ws = _new(ids, stream, (nb // 4,), _torch.int32) if nb else None
+    st = _on_stream(device, stream, (ids, offsets, place))
+    _call(device, agcn_sort_groups, n, k, groups, ids.data_ptr(), ids.element_size(), ldi,
+          offsets.data_ptr(), place.data_ptr(), ldp, ws.data_ptr() if nb else None, st)
+    return offsets, place
+
+
+def dispatch(X, place, out=None, stream=None):
+    """The rows of X (n, f), of any type, in group order: (n * k, f) with row place[t][c] = X[t],
+    and rows of ids without a group 0. Its gradient is ``combine`` of the rows' without
+    weights."""
+    (n, f), device = _first("X", X, 2)
+    k = place.shape[1] if getattr(place, "ndim", 0) == 2 else 0
+    dtype, size = X.dtype, X.element_size()
+    ldx = _matrix("X", X, device, (n, f), dtype)
+    ldp = _matrix("place", place, device, (n, k), _torch.int32)
+    if out is None:
+        if size == 1:
+            out, ldy = _new_rows(X, stream, (n * k,), f, dtype)
+        else:
+            out, ldy = _new(X, stream, (n * k, f), dtype), f
+    else:
+        ldy = _matrix("out", out, device, (n * k, f), dtype)
+    st = _on_stream(device, stream, (X, place, out))
+    _call(device, agcn_dispatch, n, k, f * size, X.data_ptr(), ldx * size, place.data_ptr(), ldp,
+          out.data_ptr(), ldy * size, st)
+    return out
+
+
+def combine(R, place, weights=None, out=None, stream=None):
+    """(n, f) with row t the sum over c of weights[t][c] R[place[t][c]], ids without a group left
+    out: R (n * k, f) float32, bfloat16 or float16 rows in group order, place (n, k) as
+    ``sort_groups`` gives it, weights (n, k) float32 or None (all 1). Added in 32 bits."""
+    (rows, f), device = _first("R", R, 2)
+    dtype = R.dtype
+    code = _dtype_code("R", dtype)
+    n, k, ldp = _places(place, device, rows)
+    ldr = _matrix("R", R, device, (rows, f), dtype)
+    w, ldw = None, k
+    if weights is not None:
+        ldw = _matrix("weights", weights, device, (n, k), _torch.float32)
+        w = weights.data_ptr()
+    if out is None:
+        out, ldy = _new(R, stream, (n, f), dtype), f
+    else:
+        ldy = _matrix("out", out, device, (n, f), dtype)
+    st = _on_stream(device, stream, (R, place, weights, out))
+    _call(device, agcn_combine, n, k, f, code, R.data_ptr(), ldr, place.data_ptr(), ldp, w, ldw,
+          out.data_ptr(), ldy, st)
+    return out
+
+
+def _places(place, device, rows):
+    """(n, k) and the row stride of the places of `rows` rows."""
+    if not isinstance(place, _torch.Tensor) or place.dim() != 2:
+        raise TypeError("place must be an (n, k) int32 CUDA tensor")
+    n, k = place.shape
+    ldp = _matrix("place", place, device, (n, k), _torch.int32)
+    if n * k != rows:
+        raise ValueError("place must name as many rows as there are")
+    return n, k, ldp
+
+
+def combine_backward(grad, R, place, weights, out=None, stream=None):
+    """Gradients of ``combine`` with weights from grad (n, f), that of its result: (dR, dweights),
+    dR (n * k, f) of R's type and dweights (n, k) float32, 0 for ids without a group. out: where dR
+    is written. (Without weights dR is ``dispatch`` of grad.)"""
+    (rows, f), device = _first("R", R, 2)
+    dtype = R.dtype
+    code = _dtype_code("R", dtype)
+    n, k, ldp = _places(place, device, rows)
+    ldr = _matrix("R", R, device, (rows, f), dtype)
+    ldg = _matrix("grad", grad, device, (n, f), dtype)
+    ldw = _matrix("weights", weights, device, (n, k), _torch.float32)
+    if out is None:
+        out, ldo = _new(R, stream, (rows, f), dtype), f
+    else:
+        ldo = _matrix("out", out, device, (rows, f), dtype)
+    dw = _new(R, stream, (n, k), _torch.float32)
+    st = _on_stream(device, stream, (grad, R, place, weights, out))
+    _call(device, agcn_combine_backward, n, k, f, code, grad.data_ptr(), ldg, R.data_ptr(), ldr,
+          place.data_ptr(), ldp, weights.data_ptr(), ldw, out.data_ptr(), ldo, dw.data_ptr(), k, st)
+    return out, dw

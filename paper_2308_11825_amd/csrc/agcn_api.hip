@@ -911,3 +911,242 @@ int agcn_grouped_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, co
 }
 
 }  // extern "C"
+
+// ---- products of 8-bit integers, layer norm, rows sent to groups ------------------
+
+namespace {
+
+int int_linear_checked(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q, int64_t ldq,
+                       const float* d_S, const void* d_WQ, int64_t ldwq, int64_t group_wq, const float* d_WS,
+                       int64_t group_ws, const int32_t* d_offsets, bool grouped, int32_t dtype, void* d_Y,
+                       int64_t ldy, void* stream, int32_t epilogue) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(fin, "fin")) return rc;
+  if (int rc = check_width(fout, "fout")) return rc;
+  if (fin > agcn::kMostIntFin) return fail(AGCN_ERR_UNSUPPORTED, "fin is over 2^17 - 1");
+  if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (grouped && (n > INT32_MAX || groups > agcn::kMostWidth))
+    return fail(AGCN_ERR_UNSUPPORTED, "over 2^31 - 1 rows or 2^24 groups");
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  if (epilogue != AGCN_EPILOGUE_NONE && epilogue != AGCN_EPILOGUE_RELU)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "epilogue must be AGCN_EPILOGUE_NONE or AGCN_EPILOGUE_RELU");
+  const bool any = n > 0 && fout > 0;  // without rows of Y nothing is read
+  Matrix m[] = {
+      {"Q", d_Q, any ? n : 0, fin, ldq, 1, false},
+      {"S", d_S, any && fin > 0 ? 1 : 0, n, n, 4, false},
+      {"WQ", d_WQ, any ? fout : 0, fin, ldwq, 1, false, groups, group_wq},
+      {"WS", d_WS, any && fin > 0 ? 1 : 0, fout, fout, 4, false, groups, group_ws},
+      {"offsets", d_offsets, any && grouped ? 1 : 0, groups + 1, groups + 1, 4, false},
+      {"Y", d_Y, any ? n : 0, fout, ldy, size, true},
+  };
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_int_linear(n, fin, fout, groups, d_Q, ldq, d_S, d_WQ, ldwq, group_wq, d_WS, group_ws,
+                              grouped ? d_offsets : nullptr, dtype, d_Y, ldy, static_cast<hipStream_t>(stream),
+                              epilogue);
+}
+
+int check_parameters(int32_t dtype, int32_t p_dtype, int64_t* size, int64_t* p_size) {
+  if (int rc = check_type(dtype, size)) return rc;
+  if (int rc = check_type(p_dtype, p_size)) return rc;
+  if (p_dtype != dtype && p_dtype != AGCN_FLOAT)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "parameters must have the rows' type or AGCN_FLOAT");
+  return AGCN_OK;
+}
+
+// n rows of k slots.
+int check_slots(int64_t n, int32_t k) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (k < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "k must be >= 0");
+  if (n > INT32_MAX || n * k > INT32_MAX) return fail(AGCN_ERR_UNSUPPORTED, "over 2^31 - 1 rows or n * k");
+  return AGCN_OK;
+}
+int check_groups(int32_t groups) {
+  if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (groups > agcn::kMostSortGroups) return fail(AGCN_ERR_UNSUPPORTED, "over 65536 groups");
+  return AGCN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int agcn_quantize_rows_int(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, void* d_Q,
+                           int64_t ldq, float* d_S, void* stream) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  Matrix m[] = {{"X", d_X, n, f, ldx, size, false}, {"Q", d_Q, n, f, ldq, 1, true}, {"S", d_S, 1, n, n, 4, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_quantize_int(n, f, dtype, d_X, ldx, d_Q, ldq, d_S, static_cast<hipStream_t>(stream));
+}
+
+int agcn_quantize_weight_int(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* d_W,
+                             int64_t ldw, int64_t group_w, void* d_Q, int64_t ldq, int64_t group_q,
+                             float* d_S, int64_t group_s, void* stream) {
+  if (groups < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "groups must be >= 0");
+  if (groups > agcn::kMostWidth) return fail(AGCN_ERR_UNSUPPORTED, "over 2^24 groups");
+  if (int rc = check_width(fin, "fin")) return rc;
+  if (int rc = check_width(fout, "fout")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  Matrix m[] = {{"W", d_W, fin, fout, ldw, size, false, groups, group_w},
+                {"Q", d_Q, fout, fin, ldq, 1, true, groups, group_q},
+                {"S", d_S, 1, fout, fout, 4, true, groups, group_s}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_quantize_weight_int(groups, fin, fout, dtype, d_W, ldw, group_w, d_Q, ldq, group_q, d_S, group_s,
+                                       static_cast<hipStream_t>(stream));
+}
+
+int agcn_int_linear(int64_t n, int32_t fin, int32_t fout, const void* d_Q, int64_t ldq, const float* d_S,
+                    const void* d_WQ, int64_t ldwq, const float* d_WS, int32_t dtype, void* d_Y,
+                    int64_t ldy, void* stream, int32_t epilogue) {
+  return int_linear_checked(n, fin, fout, 1, d_Q, ldq, d_S, d_WQ, ldwq, 0, d_WS, 0, nullptr, false, dtype, d_Y, ldy,
+                            stream, epilogue);
+}
+
+int agcn_grouped_int_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* d_Q,
+                            int64_t ldq, const float* d_S, const void* d_WQ, int64_t ldwq,
+                            int64_t group_wq, const float* d_WS, int64_t group_ws,
+                            const int32_t* d_offsets, int32_t dtype, void* d_Y, int64_t ldy,
+                            void* stream, int32_t epilogue) {
+  return int_linear_checked(n, fin, fout, groups, d_Q, ldq, d_S, d_WQ, ldwq, group_wq, d_WS, group_ws, d_offsets,
+                            true, dtype, d_Y, ldy, stream, epilogue);
+}
+
+int agcn_layer_norm(int64_t n, int32_t f, int32_t dtype, const void* d_X, int64_t ldx, const void* d_R,
+                    int64_t ldr, void* d_H, int64_t ldh, const void* d_g, const void* d_b,
+                    int32_t p_dtype, float eps, void* d_Y, int64_t ldy, float* d_stats, int64_t lds,
+                    void* stream) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0, p_size = 0;
+  if (int rc = check_parameters(dtype, p_dtype, &size, &p_size)) return rc;
+  if (!(eps > 0.0f) || eps > 3.0e38f)
+    return fail(AGCN_ERR_INVALID_ARGUMENT, "eps must be positive and finite");
+  // H on X or R: a row's values are read before they are written.
+  const bool on_x = d_H != nullptr && d_H == d_X && (ldh == ldx || n <= 1);
+  const bool on_r = d_H != nullptr && d_H == d_R && (ldh == ldr || n <= 1);
+  const int64_t rx = on_x ? 0 : n, rr = d_R != nullptr && !on_r ? n : 0, rh = d_H != nullptr ? n : 0;
+  Matrix m[] = {{"X", d_X, rx, f, ldx, size, false},
+                {"R", d_R, rr, f, d_R != nullptr ? ldr : f, size, false},
+                {"H", d_H, rh, f, d_H != nullptr ? ldh : f, size, true},
+                {"g", d_g, n > 0 ? 1 : 0, f, f, p_size, false},
+                {"b", d_b, n > 0 && d_b != nullptr ? 1 : 0, f, f, p_size, false},
+                {"Y", d_Y, n, f, ldy, size, true},
+                {"stats", d_stats, f > 0 && d_stats != nullptr ? n : 0, 2, d_stats != nullptr ? lds : 2, 4, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_layer_norm(n, f, dtype, d_X, ldx, d_R, ldr, d_H, ldh, d_g, d_b, p_dtype, eps, d_Y, ldy, d_stats,
+                              lds, static_cast<hipStream_t>(stream));
+}
+
+int agcn_layer_norm_workspace_size(int64_t n, int32_t f, int32_t dtype, size_t* bytes) {
+  if (bytes == nullptr) return fail(AGCN_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  *bytes = agcn::layer_norm_workspace_bytes(n, f, dtype);
+  return AGCN_OK;
+}
+
+int agcn_layer_norm_backward(int64_t n, int32_t f, int32_t dtype, const void* d_dY, int64_t lddy,
+                             const void* d_H, int64_t ldh, const void* d_dH, int64_t lddh,
+                             const float* d_stats, int64_t lds, const void* d_g, int32_t p_dtype,
+                             void* d_dX, int64_t lddx, void* d_dg, void* d_db, void* d_ws,
+                             void* stream) {
+  if (n < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0, p_size = 0;
+  if (int rc = check_parameters(dtype, p_dtype, &size, &p_size)) return rc;
+  const bool sums = d_dg != nullptr || d_db != nullptr;
+  const int64_t ws = sums ? (int64_t)agcn::layer_norm_workspace_bytes(n, f, dtype) : 0;
+  Matrix m[] = {{"dY", d_dY, n, f, lddy, size, false},
+                {"H", d_H, n, f, ldh, size, false},
+                {"dH", d_dH, d_dH != nullptr ? n : 0, f, d_dH != nullptr ? lddh : f, size, false},
+                {"stats", d_stats, f > 0 ? n : 0, 2, lds, 4, false},
+                {"g", d_g, n > 0 ? 1 : 0, f, f, p_size, false},
+                {"dX", d_dX, n, f, lddx, size, true},
+                {"dg", d_dg, d_dg != nullptr ? 1 : 0, f, f, p_size, true},
+                {"db", d_db, d_db != nullptr ? 1 : 0, f, f, p_size, true},
+                {"workspace", d_ws, ws > 0 ? 1 : 0, ws / 4, ws / 4, 4, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_layer_norm_backward(n, f, dtype, d_dY, lddy, d_H, ldh, d_dH, lddh, d_stats, lds, d_g, p_dtype,
+                                       d_dX, lddx, d_dg, d_db, d_ws, static_cast<hipStream_t>(stream));
+}
+
+int agcn_sort_groups_workspace_size(int64_t n, int32_t k, int32_t groups, size_t* bytes) {
+  if (bytes == nullptr) return fail(AGCN_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  if (int rc = check_slots(n, k)) return rc;
+  if (int rc = check_groups(groups)) return rc;
+  *bytes = agcn::sort_workspace_bytes(n * k, groups);
+  return AGCN_OK;
+}
+
+int agcn_sort_groups(int64_t n, int32_t k, int32_t groups, const void* d_ids, int32_t id_bytes,
+                     int64_t ldi, int32_t* d_offsets, int32_t* d_place, int64_t ldp, void* d_ws,
+                     void* stream) {
+  if (int rc = check_slots(n, k)) return rc;
+  if (int rc = check_groups(groups)) return rc;
+  if (id_bytes != 4 && id_bytes != 8) return fail(AGCN_ERR_INVALID_ARGUMENT, "id_bytes must be 4 or 8");
+  const int64_t ws = (int64_t)agcn::sort_workspace_bytes(n * k, groups);
+  Matrix m[] = {{"ids", d_ids, n, k, ldi, id_bytes, false},
+                {"offsets", d_offsets, 1, groups + 1, groups + 1, 4, true},
+                {"place", d_place, n, k, ldp, 4, true},
+                {"workspace", d_ws, ws > 0 ? 1 : 0, ws / 4, ws / 4, 4, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_sort_groups(n, k, groups, d_ids, id_bytes, ldi, d_offsets, d_place, ldp, d_ws,
+                               static_cast<hipStream_t>(stream));
+}
+
+int agcn_dispatch(int64_t n, int32_t k, int64_t bytes, const void* d_X, int64_t ldx,
+                  const int32_t* d_place, int64_t ldp, void* d_Y, int64_t ldy, void* stream) {
+  if (int rc = check_slots(n, k)) return rc;
+  if (bytes < 0) return fail(AGCN_ERR_INVALID_ARGUMENT, "bytes must be >= 0");
+  if (bytes > (int64_t)agcn::kMostWidth * 8) return fail(AGCN_ERR_UNSUPPORTED, "bytes is over 2^27");
+  const bool any = k > 0;
+  Matrix m[] = {{"X", d_X, any ? n : 0, bytes, ldx, 1, false},
+                {"place", d_place, bytes > 0 ? n : 0, k, ldp, 4, false},
+                {"Y", d_Y, n * k, bytes, ldy, 1, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_dispatch(n, k, bytes, d_X, ldx, d_place, ldp, d_Y, ldy, static_cast<hipStream_t>(stream));
+}
+
+int agcn_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* d_R, int64_t ldr,
+                 const int32_t* d_place, int64_t ldp, const float* d_W, int64_t ldw, void* d_Y,
+                 int64_t ldy, void* stream) {
+  if (int rc = check_slots(n, k)) return rc;
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  const int64_t slots = f > 0 ? n : 0;
+  Matrix m[] = {{"R", d_R, n * k, f, ldr, size, false},
+                {"place", d_place, slots, k, ldp, 4, false},
+                {"W", d_W, d_W != nullptr ? slots : 0, k, d_W != nullptr ? ldw : k, 4, false},
+                {"Y", d_Y, n, f, ldy, size, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_combine(n, k, f, dtype, d_R, ldr, d_place, ldp, d_W, ldw, d_Y, ldy,
+                           static_cast<hipStream_t>(stream));
+}
+
+int agcn_combine_backward(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* d_dY,
+                          int64_t lddy, const void* d_R, int64_t ldr, const int32_t* d_place,
+                          int64_t ldp, const float* d_W, int64_t ldw, void* d_dR, int64_t lddr,
+                          float* d_dW, int64_t lddw, void* stream) {
+  if (int rc = check_slots(n, k)) return rc;
+  if (int rc = check_width(f, "f")) return rc;
+  int64_t size = 0;
+  if (int rc = check_type(dtype, &size)) return rc;
+  Matrix m[] = {{"dY", d_dY, k > 0 ? n : 0, f, lddy, size, false},
+                {"R", d_R, n * k, f, ldr, size, false},
+                {"place", d_place, n, k, ldp, 4, false},
+                {"W", d_W, n, k, ldw, 4, false},
+                {"dR", d_dR, n * k, f, lddr, size, true},
+                {"dW", d_dW, n, k, lddw, 4, true}};
+  if (int rc = check_matrices(m)) return rc;
+  return agcn::run_combine_backward(n, k, f, dtype, d_dY, lddy, d_R, ldr, d_place, ldp, d_W, ldw, d_dR, lddr, d_dW,
+                                    lddw, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

@@ -205,6 +205,42 @@ int run_quantized_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, c
                          const int32_t* offsets, int32_t dtype, void* Y, int64_t ldy, hipStream_t st,
                          int32_t act);
 
+// Rows and weights in 8-bit integers (agcn_quant.hip) and their products
+// (agcn_ilinear.hip). Sums of 2^17 products can leave 32 bits.
+constexpr int32_t kMostIntFin = (1 << 17) - 1;
+int run_quantize_int(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, void* Q, int64_t ldq, float* S,
+                     hipStream_t st);
+int run_quantize_weight_int(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* W, int64_t ldw,
+                            int64_t group_w, void* Q, int64_t ldq, int64_t group_q, float* S, int64_t group_s,
+                            hipStream_t st);
+int run_int_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const void* A, int64_t lda, const float* SA,
+                   const void* W, int64_t ldw, int64_t group_w, const float* SW, int64_t group_sw,
+                   const int32_t* offsets, int32_t dtype, void* Y, int64_t ldy, hipStream_t st, int32_t act);
+
+// Layer norm and its gradients (agcn_norm.hip).
+size_t layer_norm_workspace_bytes(int64_t n, int32_t f, int32_t dtype);
+int run_layer_norm(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                   void* H, int64_t ldh, const void* g, const void* b, int32_t p_dtype, float eps, void* Y,
+                   int64_t ldy, float* stats, int64_t lds, hipStream_t st);
+int run_layer_norm_backward(int64_t n, int32_t f, int32_t dtype, const void* dY, int64_t lddy, const void* H,
+                            int64_t ldh, const void* dH, int64_t lddh, const float* stats, int64_t lds,
+                            const void* g, int32_t p_dtype, void* dX, int64_t lddx, void* dg, void* db, void* ws,
+                            hipStream_t st);
+
+// Rows sent to groups and back (agcn_route.hip). Groups of a sort, at most: its counts are
+// held for each of up to 256 tiles of slots.
+constexpr int32_t kMostSortGroups = 1 << 16;
+size_t sort_workspace_bytes(int64_t slots, int32_t groups);
+int run_sort_groups(int64_t n, int32_t k, int32_t groups, const void* ids, int32_t id_bytes, int64_t ldi,
+                    int32_t* offsets, int32_t* place, int64_t ldp, void* ws, hipStream_t st);
+int run_dispatch(int64_t n, int32_t k, int64_t bytes, const void* X, int64_t ldx, const int32_t* place, int64_t ldp,
+                 void* Y, int64_t ldy, hipStream_t st);
+int run_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* R, int64_t ldr, const int32_t* place,
+                int64_t ldp, const float* w, int64_t ldw, void* out, int64_t ldo, hipStream_t st);
+int run_combine_backward(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* dOut, int64_t lddo,
+                         const void* R, int64_t ldr, const int32_t* place, int64_t ldp, const float* w, int64_t ldw,
+                         void* dR, int64_t lddr, float* dw, int64_t lddw, hipStream_t st);
+
 // agcn_spmm_noalloc's workspace: a fixed device array of this many bytes in
 // agcn_spmm.hip; noalloc_scratch returns its address on `device` (the
 // current device), looked up on the first call for that device.

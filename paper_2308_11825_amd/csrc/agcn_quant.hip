@@ -18,6 +18,7 @@
 
 #include "agcn_quant.hpp"
 #include "agcn_row_tiles.hpp"
+#include "agcn_rows.hpp"
 
 namespace agcn {
 
@@ -309,9 +310,148 @@ __global__ __launch_bounds__(256) void k_quantize_weight(int32_t fin, int32_t fo
   }
 }
 
-int launched(const char* what) {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? AGCN_OK : hip_fail(e, what);
+// --- 8-bit integers ---------------------------------------------------------------
+//
+// A row (of X, or of W^T) as integers of -127 to 127 and one float: with a its largest
+// |x|, q = x (127 / a) rounded to nearest even, 127 / a and the product rounded to fp32, and
+// s = a / 127. A row that holds an infinity or NaN has s = NaN, which its results then are;
+// a row of zeros s = 0.
+
+// Bits of |v|: they order as the values do, with infinities and NaN above all numbers.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+template <int ROR>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return std::max(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x120 + ROR, 0xf, 0xf, false));
+}
+__device__ __forceinline__ uint32_t magnitude16(uint32_t v) {
+  return dpp_max<1>(dpp_max<2>(dpp_max<4>(dpp_max<8>(v))));
+}
+
+// x as an integer is rint(x up factor); up keeps 127 / a inside fp32's range.
+struct IntScale {
+  float up, factor, scale;
+  __device__ __forceinline__ explicit IntScale(uint32_t top) {
+    const float a = __builtin_bit_cast(float, top);
+    const bool number = top < 0x7f800000u;
+    up = a < 0x1p-100f ? 0x1p100f : 1.0f;
+    factor = number && a > 0.0f ? 127.0f / (a * up) : 0.0f;
+    scale = number ? a / 127.0f : __builtin_nanf("");
+  }
+  __device__ __forceinline__ uint32_t operator()(float x) const {
+    return (uint32_t)(int)rintf(x * up * factor) & 0xffu;  // (0 for NaN, and for 0 times an infinity)
+  }
+};
+
+// One row per G lanes, NV pieces of V columns a lane, in registers from the largest value to
+// the 8 bits.
+template <class T, int G, int NV, int V>
+__global__ __launch_bounds__(G > 256 ? G : 256) void k_quantize_int(int64_t n, int32_t f, const T* X, int64_t ldx,
+                                                                  int8_t* Q, int64_t ldq, float* S) {
+  constexpr int kThreads = G > 256 ? G : 256, kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
+  __shared__ uint32_t part[2][16];
+  const int lane = threadIdx.x % G;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < n; row += (int64_t)gridDim.x * kRows,
+               turn ^= 1) {
+    Piece<T, V> x[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) x[v] = load_any<Piece<T, V>>(X + row * ldx + Column<G, V>(v, lane, f).start);
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < V; ++i) top = std::max(top, magnitude(to_float(x[v].e[i])));
+    top = magnitude16(top);
+    if constexpr (G >= 32) top = std::max(top, (uint32_t)__shfl_xor((int)top, 16));
+    if constexpr (G >= 64) top = std::max(top, (uint32_t)__shfl_xor((int)top, 32));
+    if constexpr (kWaves > 1) {
+      if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = top;
+      __syncthreads();
+      top = magnitude16(part[turn][threadIdx.x % kWaves % 16]);
+    }
+    const IntScale s(top);
+    if (lane == 0) S[row] = s.scale;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const Column<G, V> c(v, lane, f);
+      if (c.shared == V) continue;
+      uint32_t q[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) q[i] = s(to_float(x[v].e[i]));
+      int8_t* to = Q + row * ldq + c.start;
+      if constexpr (V == 1) {
+        *to = (int8_t)q[0];
+      } else {
+        uint32_t w[V / 4];
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) w[i] = q[4 * i] | q[4 * i + 1] << 8 | q[4 * i + 2] << 16 | q[4 * i + 3] << 24;
+        __builtin_memcpy(to, w, V);
+      }
+    }
+  }
+}
+
+// Rows too long for registers, or of no columns: one workgroup a row, its values read twice.
+template <class T>
+__global__ __launch_bounds__(1024) void k_quantize_int_long(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* Q,
+                                                            int64_t ldq, float* S) {
+  __shared__ uint32_t part[16];
+  for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+    const T* x = X + row * ldx;
+    uint32_t top = 0;
+    for (int c = threadIdx.x; c < f; c += 1024) top = std::max(top, magnitude(to_float(x[c])));
+    top = magnitude16(top);
+    top = std::max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = std::max(top, (uint32_t)__shfl_xor((int)top, 32));
+    __syncthreads();  // the row before has been read
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
+    __syncthreads();
+    const IntScale s(magnitude16(part[threadIdx.x % 16]));
+    if (threadIdx.x == 0) S[row] = s.scale;
+    for (int c = threadIdx.x; c < f; c += 1024) Q[row * ldq + c] = (int8_t)s(to_float(x[c]));
+  }
+}
+
+// W (fin x fout) as W^T: one workgroup 64 columns of W, read once for their largest values and
+// once more to be written, 64 x 64 at a time through LDS.
+template <class T>
+__global__ __launch_bounds__(1024) void k_quantize_weight_int(int32_t fin, int32_t fout, const T* W, int64_t ldw,
+                                                              int64_t group_w, int8_t* Q, int64_t ldq,
+                                                              int64_t group_q, float* S, int64_t group_s) {
+  __shared__ uint32_t part[16][64];
+  __shared__ uint8_t tile[64][68];  // [column of W][row]
+  const int at = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t e = blockIdx.y, n0 = (int64_t)blockIdx.x * 64, n = n0 + at;
+  W += e * group_w;
+  Q += e * group_q;
+  const bool inside = n < fout;
+  uint32_t top = 0;
+  if (inside) {
+#pragma unroll 8
+    for (int k = wave; k < fin; k += 16) top = std::max(top, magnitude(to_float(W[(int64_t)k * ldw + n])));
+  }
+  part[wave][at] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) top = std::max(top, part[w][at]);
+  const IntScale s(top);
+  if (inside && wave == 0) S[e * group_s + n] = s.scale;
+  for (int k0 = 0; k0 < fin; k0 += 64) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k0 + wave * 4 + i;
+      tile[at][wave * 4 + i] = inside && k < fin ? (uint8_t)s(to_float(W[(int64_t)k * ldw + n])) : 0;
+    }
+    __syncthreads();
+    const int c = threadIdx.x / 16, k = threadIdx.x % 16 * 4;  // four values of a row of W^T
+    if (n0 + c < fout) {
+      int8_t* to = Q + (n0 + c) * ldq + k0 + k;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k0 + k + i < fin) to[i] = (int8_t)tile[c][k + i];
+    }
+    __syncthreads();
+  }
 }
 
 // Workgroups resident at once, about: rows past them are looped over, with the
@@ -365,6 +505,40 @@ int quantize_typed(int64_t n, int32_t f, const void* X, int64_t ldx, uint8_t* Q,
   return AGCN_OK;
 }
 
+template <class T, int V>
+int quantize_int_pieces(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* Q, int64_t ldq, float* S,
+                        hipStream_t st) {
+  const bool fits = f > 0 && row_shape(ceil_div64(f, V), [&](auto shape) {
+    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = G > 256 ? G : 256;
+    const int64_t grid = std::min<int64_t>(kNormGroupsShort, ceil_div64(n, kThreads / G));
+    k_quantize_int<T, G, NV, V><<<(unsigned)grid, kThreads, 0, st>>>(n, f, X, ldx, Q, ldq, S);
+  });
+  if (!fits)
+    k_quantize_int_long<T><<<(unsigned)std::min<int64_t>(kNormGroups, n), 1024, 0, st>>>(n, f, X, ldx, Q, ldq, S);
+  return launched("k_quantize_int launch");
+}
+template <class T>
+int quantize_int_typed(int64_t n, int32_t f, const void* X, int64_t ldx, void* Q, int64_t ldq, float* S,
+                       hipStream_t st) {
+  const T* x = static_cast<const T*>(X);
+  int8_t* q = static_cast<int8_t*>(Q);
+  return f < kPiece<T> ? quantize_int_pieces<T, 1>(n, f, x, ldx, q, ldq, S, st)
+                       : quantize_int_pieces<T, kPiece<T>>(n, f, x, ldx, q, ldq, S, st);
+}
+template <class T>
+int quantize_weight_int_typed(int32_t groups, int32_t fin, int32_t fout, const void* W, int64_t ldw, int64_t group_w,
+                              void* Q, int64_t ldq, int64_t group_q, float* S, int64_t group_s, hipStream_t st) {
+  constexpr int32_t kMost = 65535;  // a grid's y
+  for (int32_t e = 0; e < groups; e += kMost) {
+    const dim3 grid((unsigned)ceil_div64(fout, 64), (unsigned)std::min(kMost, groups - e));
+    k_quantize_weight_int<T><<<grid, 1024, 0, st>>>(fin, fout, static_cast<const T*>(W) + e * group_w, ldw, group_w,
+                                                    static_cast<int8_t*>(Q) + e * group_q, ldq, group_q,
+                                                    S + e * group_s, group_s);
+    if (int rc = launched("k_quantize_weight_int launch")) return rc;
+  }
+  return AGCN_OK;
+}
+
 }  // namespace
 
 int run_rms_norm(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, const void* R,
@@ -412,6 +586,25 @@ int run_quantize_weight(int32_t groups, int32_t fin, int32_t fout, int32_t dtype
     if (int rc = launched("k_quantize_weight launch")) return rc;
   }
   return AGCN_OK;
+}
+
+int run_quantize_int(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t ldx, void* Q, int64_t ldq, float* S,
+                     hipStream_t st) {
+  if (n == 0) return AGCN_OK;
+  if (dtype == AGCN_FLOAT) return quantize_int_typed<float>(n, f, X, ldx, Q, ldq, S, st);
+  if (dtype == AGCN_BFLOAT) return quantize_int_typed<bf16_t>(n, f, X, ldx, Q, ldq, S, st);
+  return quantize_int_typed<f16_t>(n, f, X, ldx, Q, ldq, S, st);
+}
+
+int run_quantize_weight_int(int32_t groups, int32_t fin, int32_t fout, int32_t dtype, const void* W, int64_t ldw,
+                            int64_t group_w, void* Q, int64_t ldq, int64_t group_q, float* S, int64_t group_s,
+                            hipStream_t st) {
+  if (groups == 0 || fout == 0) return AGCN_OK;
+  if (dtype == AGCN_FLOAT)
+    return quantize_weight_int_typed<float>(groups, fin, fout, W, ldw, group_w, Q, ldq, group_q, S, group_s, st);
+  if (dtype == AGCN_BFLOAT)
+    return quantize_weight_int_typed<bf16_t>(groups, fin, fout, W, ldw, group_w, Q, ldq, group_q, S, group_s, st);
+  return quantize_weight_int_typed<f16_t>(groups, fin, fout, W, ldw, group_w, Q, ldq, group_q, S, group_s, st);
 }
 
 }  // namespace agcn

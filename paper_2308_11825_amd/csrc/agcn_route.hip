@@ -1,0 +1,524 @@
+// Rows sent to groups (experts, types) and back.
+//
+// A row t has k slots j = t k + c, each with the id of a group. k_group_* sort the slots
+// by group, stably: place[j] = number of slots of lower groups + number of earlier slots
+// of the same group. Slots whose id is no group come after all others; their place p is
+// written as -1 - p. k_dispatch lays the rows out that way, k_combine adds them up per
+// row again, with weights, and k_combine_grad gives that sum's gradients.
+#include <algorithm>
+
+#include "agcn_rows.hpp"
+
+namespace agcn {
+
+namespace {
+
+struct SortArgs {
+  uint32_t slots;
+  int32_t k, groups;
+  const void* ids;
+  int64_t ldi;
+  int32_t* offsets;  // groups + 1
+  int32_t* place;
+  int64_t ldp;
+  int32_t* counts;  // [tiles][groups + 1], and [groups + 1] sums over the tiles
+  int32_t tiles;
+  uint32_t chunk;  // slots of a wave, whole steps of 64
+};
+
+template <class ID>
+__device__ __forceinline__ int32_t group_of(const SortArgs& a, uint32_t slot) {
+  const uint32_t t = slot / (uint32_t)a.k, c = slot % (uint32_t)a.k;
+  const ID id = static_cast<const ID*>(a.ids)[(int64_t)t * a.ldi + c];
+  return id >= 0 && id < (ID)a.groups ? (int32_t)id : a.groups;
+}
+__device__ __forceinline__ void write_place(const SortArgs& a, uint32_t slot, int32_t key, int32_t p) {
+  const uint32_t t = slot / (uint32_t)a.k, c = slot % (uint32_t)a.k;
+  a.place[(int64_t)t * a.ldp + c] = key == a.groups ? -1 - p : p;
+}
+
+// The lanes of `active` with this lane's key, of `bits` bits.
+__device__ __forceinline__ uint64_t same_key(int32_t key, uint64_t active, int bits) {
+  uint64_t same = active;
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t ones = __ballot(key >> b & 1);
+    same &= (key >> b & 1) ? ones : ~ones;
+  }
+  return same;
+}
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// What the wave's lanes wrote to LDS before is what they read after.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ int wave_scan(int v) {  // inclusive
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int up = __shfl_up(v, d);
+    if (lane >= d) v += up;
+  }
+  return v;
+}
+// Exclusive sums over the workgroup's threads, and the sum of all in *total. `part` holds
+// a value per wave.
+template <int THREADS>
+__device__ __forceinline__ int block_scan(int v, int* part, int* total) {
+  const int in = wave_scan(v), wave = threadIdx.x / 64;
+  if (threadIdx.x % 64 == 63) part[wave] = in;
+  __syncthreads();
+  int before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    before += w < wave ? part[w] : 0;
+    sum += part[w];
+  }
+  __syncthreads();
+  *total = sum;
+  return before + in - v;
+}
+
+// Few slots: one workgroup, each wave a run of the slots. A slot's rank among its wave's
+// slots of its group, then the waves' and the groups' sums.
+constexpr int kSmallBins = 1024, kSmallSteps = 8, kSmallSlots = 1024 * kSmallSteps;
+template <class ID>
+__global__ __launch_bounds__(1024) void k_group_small(SortArgs a, int bits) {
+  __shared__ int32_t count[16][kSmallBins];
+  __shared__ int part[16];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, bins = a.groups + 1;
+  for (int i = threadIdx.x; i < 16 * bins; i += 1024) count[i / bins][i % bins] = 0;
+  __syncthreads();
+  int32_t key[kSmallSteps], rank[kSmallSteps];
+  const uint32_t first = wave * a.chunk;
+#pragma unroll
+  for (int s = 0; s < kSmallSteps; ++s) {
+    const uint32_t j = first + s * 64 + lane;
+    key[s] = s * 64 < a.chunk && j < a.slots ? group_of<ID>(a, j) : -1;
+  }
+#pragma unroll
+  for (int s = 0; s < kSmallSteps; ++s) {
+    if (s * 64 >= a.chunk) break;
+    const uint64_t same = same_key(key[s], __ballot(key[s] >= 0), bits);
+    const int before = lanes_before(same), at = key[s] >= 0 ? count[wave][key[s]] : 0;
+    rank[s] = at + before;
+    wave_order();
+    if (key[s] >= 0 && before == 0) count[wave][key[s]] = at + __popcll(same);
+    wave_order();
+  }
+  __syncthreads();
+  int sum = 0;
+  if ((int)threadIdx.x < bins) {
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      const int c = count[w][threadIdx.x];
+      count[w][threadIdx.x] = sum;
+      sum += c;
+    }
+  }
+  int total;
+  const int start = block_scan<1024>(sum, part, &total);
+  if ((int)threadIdx.x < bins) {
+    a.offsets[threadIdx.x] = start;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) count[w][threadIdx.x] += start;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < kSmallSteps; ++s)
+    if (key[s] >= 0) write_place(a, first + s * 64 + lane, key[s], count[wave][key[s]] + rank[s]);
+}
+
+// Many slots, in three launches: the groups' counts in each tile of slots, their sums over
+// the tiles before, and the places. Groups are taken kBins at a time.
+constexpr int kBins = 2048, kSortThreads = 256, kSortWaves = kSortThreads / 64, kMostSortTiles = 256;
+
+template <class ID>
+__global__ __launch_bounds__(kSortThreads) void k_group_count(SortArgs a) {
+  __shared__ int32_t count[kBins];
+  const uint32_t tile = kSortWaves * a.chunk, first = blockIdx.x * tile;
+  const uint32_t end = min(a.slots, first + tile);
+  const int bins = a.groups + 1;
+  for (int base = 0; base < bins; base += kBins) {
+    const int here = min(kBins, bins - base);
+    for (int i = threadIdx.x; i < here; i += kSortThreads) count[i] = 0;
+    __syncthreads();
+    for (uint32_t j = first + threadIdx.x; j < end; j += kSortThreads) {
+      const int key = group_of<ID>(a, j) - base;
+      if (key >= 0 && key < here) atomicAdd(&count[key], 1);  // a sum of ones: any order
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < here; i += kSortThreads)
+      a.counts[(int64_t)blockIdx.x * bins + base + i] = count[i];
+    __syncthreads();
+  }
+}
+
+// 16 groups a workgroup, 16 threads for the tiles of each.
+__global__ __launch_bounds__(256) void k_group_tiles(SortArgs a) {
+  constexpr int kEach = kMostSortTiles / 16;
+  __shared__ int32_t sums[16][17];
+  const int bins = a.groups + 1, bin = blockIdx.x * 16 + threadIdx.x % 16, s = threadIdx.x / 16;
+  int32_t v[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int tile = s * kEach + i;
+    v[i] = bin < bins && tile < a.tiles ? a.counts[(int64_t)tile * bins + bin] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) sum += v[i];
+  sums[s][threadIdx.x % 16] = sum;
+  __syncthreads();
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) before += i < s ? sums[i][threadIdx.x % 16] : 0;
+  if (bin >= bins) return;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int tile = s * kEach + i;
+    if (tile < a.tiles) a.counts[(int64_t)tile * bins + bin] = before;
+    before += v[i];
+  }
+  if (s == 15) a.counts[(int64_t)a.tiles * bins + bin] = before;
+}
+
+template <class ID>
+__global__ __launch_bounds__(kSortThreads) void k_group_place(SortArgs a, int bits) {
+  __shared__ int32_t next[kSortWaves][kBins];
+  __shared__ int part[kSortWaves];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, bins = a.groups + 1;
+  const uint32_t first = (blockIdx.x * kSortWaves + wave) * a.chunk;
+  const uint32_t end = min(a.slots, first + a.chunk);
+  const int32_t* before = a.counts + (int64_t)blockIdx.x * bins;
+  const int32_t* sums = a.counts + (int64_t)a.tiles * bins;
+  int32_t start = 0;  // of the groups from `base` on
+  for (int base = 0; base < bins; base += kBins) {
+    const int here = min(kBins, bins - base);
+    for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) next[i / kBins][i % kBins] = 0;
+    __syncthreads();
+    for (uint32_t j = first + lane; j < end; j += 64) {
+      const int key = group_of<ID>(a, j) - base;
+      if (key >= 0 && key < here) atomicAdd(&next[wave][key], 1);
+    }
+    __syncthreads();
+    for (int b = 0; b < here; b += kSortThreads) {
+      const int i = b + threadIdx.x;
+      int total;
+      const int from = start + block_scan<kSortThreads>(i < here ? sums[base + i] : 0, part, &total);
+      start += total;
+      if (i < here) {
+        if (blockIdx.x == 0) a.offsets[base + i] = from;
+        int at = from + before[base + i];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+          const int c = next[w][i];
+          next[w][i] = at;
+          at += c;
+        }
+      }
+    }
+    __syncthreads();
+    for (uint32_t j0 = first; j0 < end; j0 += 64) {
+      const uint32_t j = j0 + lane;
+      const int key = j < end ? group_of<ID>(a, j) : -1, in = key - base;
+      const bool mine = key >= 0 && in >= 0 && in < here;
+      const uint64_t same = same_key(in, __ballot(mine), bits);
+      const int n = lanes_before(same), at = mine ? next[wave][in] : 0;
+      wave_order();
+      if (mine) {
+        write_place(a, j, key, at + n);
+        if (n == 0) next[wave][in] = at + __popcll(same);
+      }
+      wave_order();
+    }
+    __syncthreads();
+  }
+}
+
+// --- rows -------------------------------------------------------------------------
+
+struct RowArgs {
+  int64_t n, f;  // rows of one per token, and their columns (k_dispatch: bytes)
+  int32_t k;
+  const int32_t* place;
+  int64_t ldp;
+  const float* w;  // or NULL
+  int64_t ldw;
+  const void* X;  // of a token
+  int64_t ldx;
+  const void* R;  // of a slot, n k of them
+  int64_t ldr;
+  void* out;  // of a token, or of a slot
+  int64_t ldo;
+  float* dw;
+  int64_t lddw;
+};
+
+// The row that a place names, and whether its slot is kept; places outside the matrix name
+// row 0 and are not.
+struct Slot {
+  int64_t row;
+  bool kept, inside;
+  __device__ __forceinline__ Slot(const RowArgs& a, int64_t t, int c) {
+    const int32_t p = a.place[t * a.ldp + c], r = p < 0 ? -1 - p : p;
+    inside = r < a.n * a.k;
+    row = inside ? r : 0;
+    kept = p >= 0 && inside;
+  }
+};
+
+// The token of a group of G lanes: one for the whole wave in scalar registers.
+template <int G>
+__device__ __forceinline__ int64_t token_of(int64_t i) {
+  const int64_t t = i * (256 / G) + threadIdx.x / G;
+  if constexpr (G < 64) return t;
+  return (int64_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)t >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)t);
+}
+
+// A row read once and written k times, W bytes a lane at a time (the last piece of a
+// row ends where the row does).
+template <int W>
+struct Bytes {
+  uint8_t b[W];
+};
+template <int W, int G>
+__global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
+  const int lane = threadIdx.x % G;
+  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+    const int64_t t = token_of<G>(i);
+    if (t >= a.n) continue;
+    const uint8_t* x = static_cast<const uint8_t*>(a.X) + t * a.ldx;
+    for (int64_t at = lane * W; at < a.f; at += G * W) {
+      const int64_t from = std::min<int64_t>(at, a.f - W);
+      const Bytes<W> v = load_any<Bytes<W>>(x + from), none = {};
+      for (int c = 0; c < a.k; ++c) {
+        const Slot s(a, t, c);
+        if (s.inside) store_any(static_cast<uint8_t*>(a.out) + s.row * a.ldo + from, s.kept ? v : none);
+      }
+    }
+  }
+}
+
+// out[t] = sum over c of w[t][c] R[place[t][c]], in c's order.
+template <class T, int V, int G>
+__global__ __launch_bounds__(256) void k_combine(RowArgs a) {
+  constexpr int kAtOnce = 4;
+  using P = Piece<T, V>;
+  const int lane = threadIdx.x % G;
+  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+    const int64_t t = token_of<G>(i);
+    if (t >= a.n) continue;
+    for (int64_t at = lane * V; at < a.f; at += G * V) {
+      const int64_t from = std::min<int64_t>(at, a.f - V);
+      float sum[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+      for (int c0 = 0; c0 < a.k; c0 += kAtOnce) {
+        P v[kAtOnce];
+        float w[kAtOnce];
+        bool kept[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int c = min(c0 + u, a.k - 1);
+          const Slot s(a, t, c);
+          kept[u] = s.kept && c0 + u < a.k;
+          w[u] = a.w != nullptr ? a.w[t * a.ldw + c] : 1.0f;
+          v[u] = load_any<P>(static_cast<const T*>(a.R) + s.row * a.ldr + from);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[e] = kept[u] ? fmaf(w[u], to_float(v[u].e[e]), sum[e]) : sum[e];
+      }
+      P o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.e[e] = (T)sum[e];
+      store_any(static_cast<T*>(a.out) + t * a.ldo + from, o);
+    }
+  }
+}
+
+// dR[place[t][c]] = w[t][c] X[t] and dw[t][c] = X[t] . R[place[t][c]], X the gradient of
+// k_combine's sum. A group of lanes has a whole token, kAtOnce slots at a time.
+template <class T, int V, int G>
+__global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
+  constexpr int kAtOnce = 4;
+  using P = Piece<T, V>;
+  const int lane = threadIdx.x % G;
+  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+    const int64_t t = token_of<G>(i);
+    if (t >= a.n) continue;
+    for (int c0 = 0; c0 < a.k; c0 += kAtOnce) {
+      int64_t row[kAtOnce];
+      float w[kAtOnce], dot[kAtOnce];
+      bool kept[kAtOnce], inside[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int c = min(c0 + u, a.k - 1);
+        const Slot s(a, t, c);
+        row[u] = s.row;
+        kept[u] = s.kept;
+        inside[u] = s.inside && c0 + u < a.k;
+        w[u] = s.kept ? a.w[t * a.ldw + c] : 0.0f;
+        dot[u] = 0.0f;
+      }
+      for (int64_t at = lane * V; at < a.f; at += G * V) {
+        const int64_t from = std::min<int64_t>(at, a.f - V);
+        const int shared = (int)(at - from);
+        const P x = load_any<P>(static_cast<const T*>(a.X) + t * a.ldx + from);
+        P r[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) r[u] = load_any<P>(static_cast<const T*>(a.R) + row[u] * a.ldr + from);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          P o;
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float g = to_float(x.e[e]);
+            o.e[e] = (T)(kept[u] ? w[u] * g : 0.0f);
+            dot[u] = e >= shared ? fmaf(g, to_float(r[u].e[e]), dot[u]) : dot[u];
+          }
+          if (inside[u]) store_any(static_cast<T*>(a.out) + row[u] * a.ldo + from, o);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        float d = dot[u];
+        if constexpr (G >= 64) d += __shfl_xor(d, 32);
+        if constexpr (G >= 32) d += __shfl_xor(d, 16);
+        d = sum16(d);
+        if (lane == 0 && c0 + u < a.k) a.dw[t * a.lddw + c0 + u] = kept[u] ? d : 0.0f;
+      }
+    }
+  }
+}
+
+// Workgroups of a launch, at most; rows past them are looped over.
+constexpr int64_t kMostGroups = 1 << 20;
+template <int G>
+unsigned row_grid(int64_t n) {
+  return (unsigned)std::min<int64_t>(kMostGroups, ceil_div64(n, 256 / G));
+}
+
+int bits_of(int bins) {
+  int bits = 0;
+  while (1 << bits < bins) ++bits;
+  return bits;
+}
+
+// Tiles of a sort, and slots of a wave of each: at least 256, whole steps of 64.
+struct SortShape {
+  int32_t tiles;
+  uint32_t chunk;
+};
+SortShape sort_shape(int64_t slots) {
+  const int64_t chunk = std::max<int64_t>(256, ceil_div64(ceil_div64(slots, kMostSortTiles * kSortWaves), 64) * 64);
+  return {(int32_t)ceil_div64(slots, kSortWaves * chunk), (uint32_t)chunk};
+}
+bool sorts_small(int64_t slots, int32_t groups) { return slots <= kSmallSlots && groups < kSmallBins; }
+
+template <class ID>
+int sort_typed(SortArgs a, hipStream_t st) {
+  const int bins = a.groups + 1;
+  if (sorts_small(a.slots, a.groups)) {
+    a.chunk = (uint32_t)ceil_div64(ceil_div64(a.slots, 16), 64) * 64;
+    k_group_small<ID><<<1, 1024, 0, st>>>(a, bits_of(bins));
+    return launched("k_group_small launch");
+  }
+  const SortShape s = sort_shape(a.slots);
+  a.tiles = s.tiles;
+  a.chunk = s.chunk;
+  k_group_count<ID><<<(unsigned)a.tiles, kSortThreads, 0, st>>>(a);
+  if (int rc = launched("k_group_count launch")) return rc;
+  k_group_tiles<<<(unsigned)ceil_div64(bins, 16), 256, 0, st>>>(a);
+  if (int rc = launched("k_group_tiles launch")) return rc;
+  k_group_place<ID><<<(unsigned)a.tiles, kSortThreads, 0, st>>>(a, bits_of(std::min(bins, kBins)));
+  return launched("k_group_place launch");
+}
+
+template <class T, int V>
+int combine_pieces(const RowArgs& a, hipStream_t st) {
+  const int64_t pieces = ceil_div64(a.f, V);
+  if (pieces <= 4) k_combine<T, V, 4><<<row_grid<4>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 16) k_combine<T, V, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 64) k_combine<T, V, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else k_combine<T, V, 256><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  return launched("k_combine launch");
+}
+template <class T, int V>
+int combine_grad_pieces(const RowArgs& a, hipStream_t st) {
+  if (ceil_div64(a.f, V) <= 16) k_combine_grad<T, V, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
+  else k_combine_grad<T, V, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  return launched("k_combine_grad launch");
+}
+
+template <class T>
+int combine_typed(const RowArgs& a, bool grad, hipStream_t st) {
+  constexpr int V = kPiece<T>;
+  if (grad) return a.f < V ? combine_grad_pieces<T, 1>(a, st) : combine_grad_pieces<T, V>(a, st);
+  return a.f < V ? combine_pieces<T, 1>(a, st) : combine_pieces<T, V>(a, st);
+}
+int combine_any(const RowArgs& a, int32_t dtype, bool grad, hipStream_t st) {
+  if (dtype == AGCN_FLOAT) return combine_typed<float>(a, grad, st);
+  return dtype == AGCN_BFLOAT ? combine_typed<bf16_t>(a, grad, st) : combine_typed<f16_t>(a, grad, st);
+}
+
+template <int W>
+int dispatch_pieces(const RowArgs& a, hipStream_t st) {
+  const int64_t pieces = ceil_div64(a.f, W);
+  if (pieces <= 1) k_dispatch<W, 1><<<row_grid<1>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 4) k_dispatch<W, 4><<<row_grid<4>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 16) k_dispatch<W, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 64) k_dispatch<W, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else k_dispatch<W, 256><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  return launched("k_dispatch launch");
+}
+
+}  // namespace
+
+size_t sort_workspace_bytes(int64_t slots, int32_t groups) {
+  if (slots == 0 || sorts_small(slots, groups)) return 0;
+  return (size_t)(sort_shape(slots).tiles + 1) * ((size_t)groups + 1) * sizeof(int32_t);
+}
+
+int run_sort_groups(int64_t n, int32_t k, int32_t groups, const void* ids, int32_t id_bytes, int64_t ldi,
+                    int32_t* offsets, int32_t* place, int64_t ldp, void* ws, hipStream_t st) {
+  const SortArgs a{(uint32_t)(n * k), std::max(k, 1), groups, ids, ldi, offsets, place, ldp,
+                   static_cast<int32_t*>(ws), 0, 0};
+  return id_bytes == 8 ? sort_typed<int64_t>(a, st) : sort_typed<int32_t>(a, st);
+}
+
+int run_dispatch(int64_t n, int32_t k, int64_t bytes, const void* X, int64_t ldx, const int32_t* place, int64_t ldp,
+                 void* Y, int64_t ldy, hipStream_t st) {
+  if (n == 0 || k == 0 || bytes == 0) return AGCN_OK;
+  RowArgs a{};
+  a.n = n, a.f = bytes, a.k = k, a.place = place, a.ldp = ldp, a.X = X, a.ldx = ldx, a.out = Y, a.ldo = ldy;
+  if (bytes >= 16) return dispatch_pieces<16>(a, st);
+  return bytes >= 4 ? dispatch_pieces<4>(a, st) : dispatch_pieces<1>(a, st);
+}
+
+int run_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* R, int64_t ldr, const int32_t* place,
+                int64_t ldp, const float* w, int64_t ldw, void* out, int64_t ldo, hipStream_t st) {
+  if (n == 0 || f == 0) return AGCN_OK;
+  RowArgs a{};
+  a.n = n, a.f = f, a.k = k, a.place = place, a.ldp = ldp, a.w = w, a.ldw = ldw, a.R = R, a.ldr = ldr;
+  a.out = out, a.ldo = ldo;
+  return combine_any(a, dtype, false, st);
+}
+
+int run_combine_backward(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* dOut, int64_t lddo,
+                         const void* R, int64_t ldr, const int32_t* place, int64_t ldp, const float* w, int64_t ldw,
+                         void* dR, int64_t lddr, float* dw, int64_t lddw, hipStream_t st) {
+  if (n == 0 || k == 0) return AGCN_OK;
+  RowArgs a{};
+  a.n = n, a.f = f, a.k = k, a.place = place, a.ldp = ldp, a.w = w, a.ldw = ldw, a.X = dOut, a.ldx = lddo;
+  a.R = R, a.ldr = ldr, a.out = dR, a.ldo = lddr, a.dw = dw, a.lddw = lddw;
+  return combine_any(a, dtype, true, st);
+}
+
+}  // namespace agcn
