@@ -63,19 +63,26 @@ __device__ __forceinline__ bool finish_stats(float s2, float over, float eps, Ro
   return s2 <= FLT_MAX && var <= FLT_MAX;
 }
 
+__device__ __forceinline__ float first_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
 // Mean and variance of h scale over a row: around the wave's own mean, whose rounding is
-// put right by the sum of the differences, and the waves' sums then joined.
+// put right by the sum of the differences, and the waves' sums then joined. That mean is
+// itself the first value and the mean difference to it, so values that are all the same
+// have no differences.
 template <int G, int NV, int V>
 __device__ __forceinline__ bool row_stats(const float (&h)[NV][V], const int (&shared)[NV], int f, float scale,
                                           float eps, float (*part)[4], RowStats* to) {
   constexpr int kWaves = G > 64 ? G / 64 : 1;
   const int own = kWaves > 1 ? wave_columns<G, NV, V>(threadIdx.x / 64, f) : f;
+  const float first = (G >= 64 ? first_lane(h[0][0]) : __shfl(h[0][0], 0, G < 64 ? G : 64)) * scale;
   float s = 0.0f;
 #pragma unroll
   for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int i = 0; i < V; ++i) s += i >= shared[v] ? h[v][i] * scale : 0.0f;
-  const float m = lanes_sum<G>(s) / (float)max(own, 1);
+    for (int i = 0; i < V; ++i) s += i >= shared[v] ? fmaf(h[v][i], scale, -first) : 0.0f;
+  const float m = first + lanes_sum<G>(s) / (float)max(own, 1);
   float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
   for (int v = 0; v < NV; ++v)
@@ -222,12 +229,13 @@ __global__ __launch_bounds__(1024) void k_layer_norm_long(NormArgs a) {
     };
     const float over = 1.0f / (float)a.f;
     auto stats = [&](float scale, RowStats* to) {
+      const float first = (to_float(x[0]) + (a.R != nullptr ? to_float(r[0]) : 0.0f)) * scale;
       float s = 0.0f;
       each([&](int64_t, int valid, const float(&h)[V]) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s += h[i] * scale;
+        for (int i = 0; i < V; ++i) s += i < valid ? fmaf(h[i], scale, -first) : 0.0f;
       });
-      const float m = block_sum(s, 0) * over;
+      const float m = first + block_sum(s, 0) * over;
       float s1 = 0.0f, s2 = 0.0f;
       each([&](int64_t, int valid, const float(&h)[V]) {
 #pragma unroll

@@ -154,7 +154,13 @@ struct Scales {
   __device__ __forceinline__ float row(int m) const { return P == kInteger && a != nullptr ? a[m] : 0.0f; }
   __device__ __forceinline__ float column(int n) const { return P == kInteger && a != nullptr ? w[n] : 0.0f; }
   static __device__ __forceinline__ float apply(Sum<P> v, float row, float column) {
-    if constexpr (P == kInteger) return (float)v * row * column;
+    if constexpr (P == kInteger) {
+      // Rounded to fp32 before the rounding to the type: some kernels' code would do both at
+      // once, and a result would depend on the shape.
+      float r = (float)v * row * column;
+      asm("" : "+v"(r));
+      return r;
+    }
     return v;
   }
 };

@@ -1,0 +1,235 @@
+"""Rows sorted by group, laid out and added up again, and the gradients of that.
+
+Sorting and laying out are exact. A sum of k terms in 32 bits is off by k u of the sum of their
+sizes (u = 2^-24), and a dot product of f columns, f / 64 + 8 of them one after the other in
+a lane and the lanes in 6 steps, by (f / 64 + 16) u of it; then comes the rounding to the type."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_2308_11825_amd as agcn  # noqa: E402
+from routed_helpers import (TYPES, U, combine, dispatch, gen, half_step, padded, randn, rows_of, sort,  # noqa: E402
+                            tiniest)
+
+DEV = "cuda:0"
+
+
+def make_ids(n, k, groups, dropped=0.1, dtype=torch.int32, seed=0):
+    g = gen(n, k, groups, seed)
+    ids = torch.randint(0, max(groups, 1), (n, k), generator=g, device=DEV)
+    out = torch.rand((n, k), generator=g, device=DEV) < dropped
+    other = torch.where(torch.rand((n, k), generator=g, device=DEV) < 0.5, -1, groups)
+    return torch.where(out, other, ids).to(dtype)
+
+
+def check_sort(ids, groups):
+    offsets, place = agcn.sort_groups(ids, groups)
+    want = sort(ids, groups)
+    assert offsets.dtype == place.dtype == torch.int32
+    assert torch.equal(offsets, want[0]) and torch.equal(place, want[1])
+    return offsets, place
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+@pytest.mark.parametrize("n,k,groups", [
+    (1, 1, 1), (1, 8, 64), (63, 1, 3), (64, 1, 2), (65, 1, 70), (48, 4, 64), (1000, 1, 1), (333, 3, 1023),
+    (333, 3, 1024), (8192, 1, 20), (8193, 1, 20), (1024, 8, 1023), (2731, 3, 5), (5000, 2, 2047), (5000, 2, 2048),
+    (5000, 2, 2049), (3000, 10, 5000), (20, 2, 65536), (60000, 2, 7), (40000, 8, 128), (5, 3, 0)])
+def test_sort(n, k, groups, dtype):
+    check_sort(make_ids(n, k, groups, dtype=dtype), groups)
+
+
+def test_sort_many_slots():
+    """More than 1024 a wave: 2.5 million slots, checked with torch's stable sort."""
+    n, k, groups = 250000, 10, 300
+    ids = make_ids(n, k, groups)
+    offsets, place = agcn.sort_groups(ids, groups)
+    key = torch.where((ids >= 0) & (ids < groups), ids, groups).reshape(-1)
+    key, order = torch.sort(key, stable=True)
+    at = torch.arange(n * k, device=DEV, dtype=torch.int32)
+    want = torch.empty_like(at)
+    want[order] = torch.where(key < groups, at, -1 - at)
+    assert torch.equal(place.reshape(-1), want)
+    assert torch.equal(offsets.long(), torch.searchsorted(key, torch.arange(groups + 1, device=DEV, dtype=torch.int32)))
+
+
+def test_sort_one_group_has_all_none_or_one():
+    for n in (700, 20000):
+        for value, groups in ((0, 5), (4, 5), (-1, 5), (7, 5), (2047, 4000), (3999, 4000)):
+            check_sort(torch.full((n, 1), value, dtype=torch.int32, device=DEV), groups)
+
+
+def test_ids_of_64_bits_are_not_cut():
+    ids = torch.tensor([[2 ** 32, 1], [-2 ** 32, 2 ** 62], [-2 ** 63, 0], [2 ** 32 + 1, 2]], device=DEV)
+    check_sort(ids, 3)
+
+
+def test_sort_strides_and_given_outputs():
+    for n in (100, 9000):
+        ids = make_ids(n, 3, 12)
+        want = agcn.sort_groups(ids, 12)
+        wide = torch.full((n, 7), 5, dtype=torch.int32, device=DEV)
+        wide[:, 2:5] = ids
+        place = torch.full((n, 5), 77, dtype=torch.int32, device=DEV)
+        offsets = torch.full((15,), 77, dtype=torch.int32, device=DEV)
+        got = agcn.sort_groups(wide[:, 2:5], 12, out=(offsets[1:14], place[:, 1:4]))
+        assert torch.equal(got[0], want[0]) and torch.equal(place[:, 1:4], want[1])
+        assert place[:, 0].eq(77).all() and place[:, 4].eq(77).all() and offsets[0] == 77 and offsets[14] == 77
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("f", [1, 2, 3, 4, 7, 8, 9, 17, 33, 64, 130, 256, 511, 601, 1024, 2048, 2049, 5000])
+def test_rows_there_and_back(f, dtype):
+    dtype, n, k, groups = TYPES[dtype], 77, 5, 9
+    ids = make_ids(n, k, groups, seed=f)
+    ids[3], ids[5] = -1, 4  # a row of no group, and one with the same group in all slots
+    _, place = agcn.sort_groups(ids, groups)
+    X = randn((n, f), dtype, 1)
+    R = agcn.dispatch(X, place)
+    assert torch.equal(R, dispatch(X, place))
+    R = randn((n * k, f), dtype, 2)
+    row, kept = rows_of(place)
+    R[row[~kept]] = float("nan")  # rows that do not count
+    w = randn((n, k), torch.float32, 3)
+    w[~kept] = float("inf")
+    ones = torch.ones_like(w)
+    for weights in (w, None):
+        out = agcn.combine(R, place, weights)
+        want, size = combine(R, place, ones if weights is None else w)
+        off = k * U * size
+        off = off + half_step(dtype) * (want.abs() + off) + tiniest(dtype)
+        assert bool(((out.double() - want).abs() <= off).all())
+    assert not out[3].any()
+    grad = randn((n, f), dtype, 4)
+    dR, dw = agcn.combine_backward(grad, R, place, w)
+    want = torch.where(kept, w, torch.zeros_like(w)).double()
+    for c in range(k):
+        exact = want[:, c, None] * grad.double()
+        off = half_step(dtype) * (1 + U) * exact.abs() + U * exact.abs() + tiniest(dtype)
+        assert bool(((dR[row[:, c]].double() - exact).abs() <= off).all())
+        terms = grad.double() * torch.where(kept[:, c, None], R[row[:, c]], torch.zeros_like(grad)).double()
+        off = (f / 64 + 16) * U * terms.abs().sum(1) + 2 ** -149
+        assert bool(((dw[:, c].double() - terms.sum(1)).abs() <= off).all())
+    assert not dR[row[~kept]].any() and not dw[~kept].any()
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 8, 9, 16])
+def test_slots_per_row(k):
+    n, f = 40, 96
+    _, place = agcn.sort_groups(make_ids(n, k, 6), 6)
+    R, w, grad = randn((n * k, f), torch.float32, 1), randn((n, k), torch.float32, 2), randn((n, f), torch.float32, 3)
+    want, size = combine(R, place, w)
+    assert bool(((agcn.combine(R, place, w).double() - want).abs() <= (k + 1) * U * size + 2 ** -149).all())
+    dR, dw = agcn.combine_backward(grad, R, place, w)
+    row, kept = rows_of(place)
+    assert torch.equal(dR[row], torch.where(kept, w, torch.zeros_like(w))[..., None] * grad[:, None])
+    dots = torch.where(kept, (R[row].double() * grad.double()[:, None]).sum(2), torch.zeros_like(w).double())
+    size = (R[row].double() * grad.double()[:, None]).abs().sum(2)
+    assert bool(((dw.double() - dots).abs() <= (f / 64 + 16) * U * size).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.int8, torch.uint8, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.bool,
+                                   torch.float64, torch.int64])
+@pytest.mark.parametrize("f", [1, 3, 5, 15, 16, 17, 100, 601, 5000])
+def test_rows_of_any_type(f, dtype):
+    n, k = 50, 3
+    _, place = agcn.sort_groups(make_ids(n, k, 8), 8)
+    size = torch.empty((), dtype=dtype).element_size()
+    raw = torch.randint(0, 2 if dtype == torch.bool else 256, (n, f * size), generator=gen(f, size), device=DEV).to(torch.uint8)
+    R = agcn.dispatch(raw.view(dtype), place)
+    assert R.dtype == dtype and R.shape == (n * k, f)
+    assert torch.equal(R.contiguous().view(torch.uint8), dispatch(raw, place))
+
+
+def test_strides_and_given_outputs():
+    for f, dtype in ((7, torch.float32), (200, torch.bfloat16), (601, torch.float16)):
+        n, k = 60, 4
+        _, place = agcn.sort_groups(make_ids(n, k, 8), 8)
+        X, R, w = randn((n, f), dtype, 1), randn((n * k, f), dtype, 2), randn((n, k), torch.float32, 3)
+        p = padded(place, 2, 1)
+        to = padded(torch.zeros_like(R), 3, 1)
+        assert agcn.dispatch(padded(X, 1, 1), p, out=to) is to and torch.equal(to, dispatch(X, place))
+        assert torch.isnan(to._base).sum() == to._base.numel() - to.numel()
+        out = padded(torch.zeros_like(X), 1)
+        assert agcn.combine(padded(R, 5, 1), p, padded(w, 1), out=out) is out
+        assert torch.equal(out, agcn.combine(R, place, w))
+        dR, dw = agcn.combine_backward(padded(X, 3), padded(R, 1, 1), p, padded(w, 3, 1), out=to)
+        want = agcn.combine_backward(X, R, place, w)
+        assert dR is to and torch.equal(dR, want[0]) and torch.equal(dw, want[1])
+
+
+def test_places_that_name_no_row_are_not_followed():
+    """Places from elsewhere: outside the matrix they are left out, and nothing else is."""
+    n, k, f = 20, 2, 48
+    _, place = agcn.sort_groups(make_ids(n, k, 4, dropped=0.0), 4)
+    bad = place.clone()
+    bad[3, 0], bad[7, 1], bad[8, 0] = n * k, 2 ** 31 - 1, -2 ** 31
+    X, R, w = randn((n, f), torch.float32, 1), randn((n * k, f), torch.float32, 2), randn((n, k), torch.float32, 3)
+    to = torch.full((n * k, f), 7.0, device=DEV)
+    agcn.dispatch(X, bad, out=to)
+    want = dispatch(X, place)
+    want[place[[3, 7, 8], [0, 1, 0]].long()] = 7.0
+    assert torch.equal(to, want)
+    w0 = w.clone()
+    w0[[3, 7, 8], [0, 1, 0]] = 0
+    assert torch.equal(agcn.combine(R, bad, w), agcn.combine(R, place, w0))
+    _, dw = agcn.combine_backward(X, R, bad, w, out=to)
+    assert not dw[[3, 7, 8], [0, 1, 0]].any()
+
+
+def test_empty():
+    X, off = torch.zeros((0, 8), device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    offsets, place = agcn.sort_groups(torch.zeros((0, 2), dtype=torch.int32, device=DEV), 3)
+    assert torch.equal(offsets, off)
+    R = agcn.dispatch(X, place)
+    assert R.shape == (0, 8) and agcn.combine(R, place).shape == (0, 8)
+    offsets, place = agcn.sort_groups(torch.zeros((5, 0), dtype=torch.int32, device=DEV), 3)
+    assert torch.equal(offsets, off) and place.shape == (5, 0)
+    X = torch.ones((5, 8), device=DEV)
+    R = agcn.dispatch(X, place)
+    assert R.shape == (0, 8) and not agcn.combine(R, place).any()
+    dR, dw = agcn.combine_backward(X, R, place, torch.zeros((5, 0), device=DEV))
+    assert dR.shape == (0, 8) and dw.shape == (5, 0)
+    _, place = agcn.sort_groups(torch.zeros((5, 2), dtype=torch.int32, device=DEV), 3)
+    dR, dw = agcn.combine_backward(X[:, :0], X[:, :0].repeat(2, 1), place, torch.ones((5, 2), device=DEV))
+    assert dR.shape == (10, 0) and not dw.any()
+
+
+def test_gradients_against_differences():
+    """combine is linear in the rows and in the weights: its differences are exact up to the
+    kernels' own roundings."""
+    n, k, f = 30, 3, 50
+    _, place = agcn.sort_groups(make_ids(n, k, 5), 5)
+    R, w, grad = randn((n * k, f), torch.float32, 1), randn((n, k), torch.float32, 2), randn((n, f), torch.float32, 3)
+    dR, dw = agcn.combine_backward(grad, R, place, w)
+    tR, tw = randn((n * k, f), torch.float32, 4), randn((n, k), torch.float32, 5)
+    up, size = combine(tR, place, w)
+    assert abs((up * grad.double()).sum() - (dR.double() * tR.double()).sum()) <= 4 * U * (size * grad.double().abs()).sum()
+    up, size = combine(R, place, tw)
+    assert abs((up * grad.double()).sum() - (dw.double() * tw.double()).sum()) <= 32 * U * (size * grad.double().abs()).sum()
+    # and combine without weights is dispatch's gradient
+    X = randn((n, f), torch.float32, 6)
+    lhs = (dispatch(X, place).double() * tR.double()).sum()
+    back = agcn.combine(tR, place).double()
+    size = combine(tR, place, torch.ones_like(w))[1]
+    assert abs(lhs - (back * X.double()).sum()) <= 8 * U * (size * X.double().abs()).sum()
+
+
+def test_far_rows():
+    """Rows past 2^32 bytes: offsets in 64 bits."""
+    n, k, f = 300000, 8, 1024
+    ids = make_ids(n, k, 16, dropped=0.0)
+    _, place = agcn.sort_groups(ids, 16)
+    X = randn((n, f), torch.bfloat16, 1)
+    R = agcn.dispatch(X, place)
+    for t in (0, 1, n // 2, n - 2, n - 1):
+        assert torch.equal(R[place[t].long()], X[t].expand(k, f))
+    del X
+    out = agcn.combine(R, place)
+    t = torch.tensor([0, 5, n // 3, n - 1], device=DEV)
+    want = R[place[t].long()].double().sum(1)
+    assert bool(((out[t].double() - want).abs() <= 2 * half_step(torch.bfloat16) * want.abs()).all())
+    w = torch.ones((n, k), device=DEV)
+    R, dw = agcn.combine_backward(out, R, place, w)
+    assert torch.equal(R[place[n - 1].long()], out[n - 1].expand(k, f))
