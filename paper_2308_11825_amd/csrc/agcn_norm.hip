@@ -128,10 +128,10 @@ __device__ __forceinline__ void write_stats(float* to, const RowStats& s, float 
 
 // One row per G lanes, NV pieces of V columns a lane (V <= f <= G * NV * V, or V = 1); the
 // parameters of its columns stay in registers too.
-template <class T, class TP, int G, int NV, int V>
-__global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm(NormArgs a) {
-  constexpr int kThreads = G > 256 ? G : 256, kRows = kThreads / G;
-  constexpr bool kKeep = NV * V <= 24 && (G < 1024 || NV == 1);
+template <class T, class TP, int G, int NV, int V, bool PAST>
+__global__ __launch_bounds__(row_threads(G)) void k_layer_norm(NormArgs a) {
+  constexpr int kThreads = row_threads(G), kRows = kThreads / G;
+  constexpr bool kKeep = G < 1024 || NV == 1;
   using In = Piece<T, V>;
   using Param = Piece<TP, V>;
   __shared__ float part[4][16][4];
@@ -161,12 +161,12 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm(NormArgs a) {
     In raw[NV];
     float h[NV][V];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) raw[v] = load_any<In>(x + start[v]);
+    for (int v = 0; v < NV; ++v) raw[v] = load_row<In, PAST>(x + start[v]);
     if (a.R != nullptr) {
       const T* r = static_cast<const T*>(a.R) + row * a.ldr;
       In add[NV];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) add[v] = load_any<In>(r + start[v]);
+      for (int v = 0; v < NV; ++v) add[v] = load_row<In, PAST>(r + start[v]);
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -191,12 +191,12 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm(NormArgs a) {
         In o;
 #pragma unroll
         for (int i = 0; i < V; ++i) o.e[i] = (T)h[v][i];
-        store_any(static_cast<T*>(a.H) + row * a.ldh + start[v], o);
+        store_row<PAST>(static_cast<T*>(a.H) + row * a.ldh + start[v], o);
       }
       In o;
 #pragma unroll
       for (int i = 0; i < V; ++i) o.e[i] = (T)fmaf(s(h[v][i]), to_float(g[v].e[i]), to_float(b[v].e[i]));
-      store_any(y + start[v], o);
+      store_row<PAST>(y + start[v], o);
     }
   }
 }
@@ -300,9 +300,9 @@ struct Normalised {
 
 // Rows as in k_layer_norm, each workgroup over every gridDim.x-th; the columns' sums stay in
 // registers until the end.
-template <class T, class TP, int G, int NV, int V>
-__global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm_grad(GradArgs a) {
-  constexpr int kThreads = G > 256 ? G : 256, kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
+template <class T, class TP, int G, int NV, int V, bool PAST>
+__global__ __launch_bounds__(row_threads(G)) void k_layer_norm_grad(GradArgs a) {
+  constexpr int kThreads = row_threads(G), kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
   using In = Piece<T, V>;
   using Param = Piece<TP, V>;
   __shared__ float part[2][16][2];
@@ -328,12 +328,12 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm_grad(GradArgs 
     In dy[NV], h[NV], dh[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      dy[v] = load_any<In>(static_cast<const T*>(a.dY) + row * a.lddy + start[v]);
-      h[v] = load_any<In>(static_cast<const T*>(a.H) + row * a.ldh + start[v]);
+      dy[v] = load_row<In, PAST>(static_cast<const T*>(a.dY) + row * a.lddy + start[v]);
+      h[v] = load_row<In, PAST>(static_cast<const T*>(a.H) + row * a.ldh + start[v]);
     }
     if (a.dH != nullptr) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) dh[v] = load_any<In>(static_cast<const T*>(a.dH) + row * a.lddh + start[v]);
+      for (int v = 0; v < NV; ++v) dh[v] = load_row<In, PAST>(static_cast<const T*>(a.dH) + row * a.lddh + start[v]);
     }
     const Normalised norm(a.stats + row * a.lds);
     float s1 = 0.0f, s2 = 0.0f;
@@ -373,20 +373,29 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm_grad(GradArgs 
         if (a.dH != nullptr) d += to_float(dh[v].e[i]);
         o.e[i] = (T)d;
       }
-      store_any(static_cast<T*>(a.dX) + row * a.lddx + start[v], o);
+      store_row<PAST>(static_cast<T*>(a.dX) + row * a.lddx + start[v], o);
     }
   }
   if (a.part == nullptr) return;
   float* to = a.part + (int64_t)blockIdx.x * 2 * a.f;
   if constexpr (kRows == 1) {
+    struct Sums {
+      float s[V];
+    };
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+      if (shared[v] == 0) {
+        store_any(to + start[v], __builtin_bit_cast(Sums, dg[v]));
+        store_any(to + a.f + start[v], __builtin_bit_cast(Sums, db[v]));
+      } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i >= shared[v]) {
-          to[start[v] + i] = dg[v][i];
-          to[a.f + start[v] + i] = db[v][i];
-        }
+        for (int i = 0; i < V; ++i)
+          if (i >= shared[v]) {
+            to[start[v] + i] = dg[v][i];
+            to[a.f + start[v] + i] = db[v][i];
+          }
+      }
+    }
   } else {
     // The rows of a wave, and then the waves in their order.
     constexpr int kWidth = G * NV * V;
@@ -398,6 +407,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_layer_norm_grad(GradArgs 
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           float x = k == 0 ? dg[v][i] : db[v][i];
+          if constexpr (G < 8) x += __shfl_xor(x, 4);
+          if constexpr (G < 16) x += __shfl_xor(x, 8);
           if constexpr (G < 32) x += __shfl_xor(x, 16);
           if constexpr (G < 64) x += __shfl_xor(x, 32);
           if (threadIdx.x % 64 < G) sums[threadIdx.x / 64][(v * V + i) * G + lane] = x;
@@ -492,15 +503,21 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(int32_t parts, int32_t
   }
 }
 
-// Workgroups resident at once, about: rows past them are looped over.
-constexpr int64_t kNormGroups = 2048, kGradGroups = 1024, kLongRowGroups = 1024;
+// Workgroups of a launch, at most; rows past them are looped over. Where rows start on lines, one
+// for every few rows (50,000 x 2048 bfloat16 134 us, and 150 with 2048 workgroups), unless
+// the parameters (over 2^15 bytes) are better kept in registers over several rows than read
+// again (32768 x 8192 bfloat16 381 us, and 439). Other rows share lines, which L2 puts together as long as
+// they are written close by: 60,000 x 601 float16 66 us, 72 with a workgroup for every row.
+constexpr int64_t kNormGroups = 1024, kSharedGroups = 8192, kMostNormGroups = 1 << 20, kLongRowGroups = 1024;
 
-template <class T, class TP, int V>
+template <class T, class TP, int V, bool PAST>
 int norm_pieces(const NormArgs& a, hipStream_t st) {
-  const bool fits = row_shape(ceil_div64(a.f, V), [&](auto shape) {
-    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = G > 256 ? G : 256;
-    const int64_t grid = std::min<int64_t>(kNormGroups, ceil_div64(a.n, kThreads / G));
-    k_layer_norm<T, TP, G, NV, V><<<(unsigned)grid, kThreads, 0, st>>>(a);
+  const bool wide = 2 * (int64_t)a.f * (int64_t)sizeof(TP) > 32768;
+  const int64_t most = !PAST ? kSharedGroups : wide ? kNormGroups : kMostNormGroups;
+  const bool fits = row_shape<V == 1, false>(ceil_div64(a.f, V), [&](auto shape) {
+    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = row_threads(G);
+    const int64_t grid = std::min<int64_t>(most, ceil_div64(a.n, kThreads / G));
+    k_layer_norm<T, TP, G, NV, V, PAST><<<(unsigned)grid, kThreads, 0, st>>>(a);
   });
   if (!fits) k_layer_norm_long<T, TP><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
   return launched("k_layer_norm launch");
@@ -508,26 +525,31 @@ int norm_pieces(const NormArgs& a, hipStream_t st) {
 
 template <class T, class TP>
 int norm_typed(const NormArgs& a, hipStream_t st) {
-  return a.f < kPiece<T> ? norm_pieces<T, TP, 1>(a, st) : norm_pieces<T, TP, kPiece<T>>(a, st);
+  if (a.f < kPiece<T>) return norm_pieces<T, TP, 1, false>(a, st);
+  const bool past = on_lines(a.X, a.ldx, sizeof(T)) && on_lines(a.R, a.ldr, sizeof(T)) &&
+                    on_lines(a.H, a.ldh, sizeof(T)) && on_lines(a.Y, a.ldy, sizeof(T));
+  return past ? norm_pieces<T, TP, kPiece<T>, true>(a, st) : norm_pieces<T, TP, kPiece<T>, false>(a, st);
 }
 
-// Workgroups whose column sums are kept apart.
+// Workgroups of the gradients, whose column sums are kept apart: two or one a compute unit, and
+// at least two steps of rows each (230,000 x 128 float32 76 us with 512 workgroups, 92 with 1024, 105 with
+// 256; 8192 x 16384 float16 190 with 256 and 223 with 512).
 int64_t grad_groups(int64_t n, int32_t f, int64_t v) {
   int64_t groups = 0;
-  if (row_shape(ceil_div64(f, v), [&](auto shape) {
-        constexpr int G = decltype(shape)::kG, kRows = (G > 256 ? G : 256) / G;
-        groups = std::min<int64_t>(kGradGroups, ceil_div64(n, kRows));
+  if (row_shape<false, true>(ceil_div64(f, v), [&](auto shape) {
+        constexpr int G = decltype(shape)::kG, kRows = row_threads(G) / G;
+        groups = std::min<int64_t>(G == 1024 ? 256 : 512, ceil_div64(n, 2 * kRows));
       }))
     return groups;
-  return std::min<int64_t>(n, std::max<int64_t>(1, kGradGroups * 2 / ceil_div64(f, 256)));
+  return std::min<int64_t>(n, std::max<int64_t>(1, 2048 / ceil_div64(f, 256)));
 }
 
-template <class T, class TP, int V>
+template <class T, class TP, int V, bool PAST>
 int grad_pieces(const GradArgs& a, TP* dg, TP* db, hipStream_t st) {
   const int64_t groups = grad_groups(a.n, a.f, V);
-  const bool fits = row_shape(ceil_div64(a.f, V), [&](auto shape) {
-    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = G > 256 ? G : 256;
-    k_layer_norm_grad<T, TP, G, NV, V><<<(unsigned)groups, kThreads, 0, st>>>(a);
+  const bool fits = row_shape<V == 1, true>(ceil_div64(a.f, V), [&](auto shape) {
+    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV;
+    k_layer_norm_grad<T, TP, G, NV, V, PAST><<<(unsigned)groups, row_threads(G), 0, st>>>(a);
   });
   if (!fits) {
     k_layer_norm_grad_long<T, TP><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
@@ -545,7 +567,10 @@ int grad_pieces(const GradArgs& a, TP* dg, TP* db, hipStream_t st) {
 template <class T, class TP>
 int grad_typed(const GradArgs& a, void* dg, void* db, hipStream_t st) {
   TP *g = static_cast<TP*>(dg), *b = static_cast<TP*>(db);
-  return a.f < kPiece<T> ? grad_pieces<T, TP, 1>(a, g, b, st) : grad_pieces<T, TP, kPiece<T>>(a, g, b, st);
+  if (a.f < kPiece<T>) return grad_pieces<T, TP, 1, false>(a, g, b, st);
+  const bool past = on_lines(a.dY, a.lddy, sizeof(T)) && on_lines(a.H, a.ldh, sizeof(T)) &&
+                    on_lines(a.dH, a.lddh, sizeof(T)) && on_lines(a.dX, a.lddx, sizeof(T));
+  return past ? grad_pieces<T, TP, kPiece<T>, true>(a, g, b, st) : grad_pieces<T, TP, kPiece<T>, false>(a, g, b, st);
 }
 
 template <class TP>

@@ -319,9 +319,13 @@ __global__ __launch_bounds__(256) void k_quantize_weight(int32_t fin, int32_t fo
 
 // Bits of |v|: they order as the values do, with infinities and NaN above all numbers.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max_xor(uint32_t v) {
+  return std::max(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false));
+}
 template <int ROR>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
-  return std::max(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x120 + ROR, 0xf, 0xf, false));
+  return dpp_max_xor<0x120 + ROR>(v);
 }
 __device__ __forceinline__ uint32_t magnitude16(uint32_t v) {
   return dpp_max<1>(dpp_max<2>(dpp_max<4>(dpp_max<8>(v))));
@@ -345,9 +349,9 @@ struct IntScale {
 // One row per G lanes, NV pieces of V columns a lane, in registers from the largest value to
 // the 8 bits.
 template <class T, int G, int NV, int V>
-__global__ __launch_bounds__(G > 256 ? G : 256) void k_quantize_int(int64_t n, int32_t f, const T* X, int64_t ldx,
+__global__ __launch_bounds__(row_threads(G)) void k_quantize_int(int64_t n, int32_t f, const T* X, int64_t ldx,
                                                                   int8_t* Q, int64_t ldq, float* S) {
-  constexpr int kThreads = G > 256 ? G : 256, kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
+  constexpr int kThreads = row_threads(G), kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
   __shared__ uint32_t part[2][16];
   const int lane = threadIdx.x % G;
   int turn = 0;
@@ -361,7 +365,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_quantize_int(int64_t n, i
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int i = 0; i < V; ++i) top = std::max(top, magnitude(to_float(x[v].e[i])));
-    top = magnitude16(top);
+    if constexpr (G == 4) top = dpp_max_xor<0x4e>(dpp_max_xor<0xb1>(top));
+    else if constexpr (G == 8) top = dpp_max_xor<0x141>(dpp_max_xor<0x4e>(dpp_max_xor<0xb1>(top)));
+    else top = magnitude16(top);
     if constexpr (G >= 32) top = std::max(top, (uint32_t)__shfl_xor((int)top, 16));
     if constexpr (G >= 64) top = std::max(top, (uint32_t)__shfl_xor((int)top, 32));
     if constexpr (kWaves > 1) {
@@ -508,8 +514,8 @@ int quantize_typed(int64_t n, int32_t f, const void* X, int64_t ldx, uint8_t* Q,
 template <class T, int V>
 int quantize_int_pieces(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* Q, int64_t ldq, float* S,
                         hipStream_t st) {
-  const bool fits = f > 0 && row_shape(ceil_div64(f, V), [&](auto shape) {
-    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = G > 256 ? G : 256;
+  const bool fits = f > 0 && row_shape<V == 1, false>(ceil_div64(f, V), [&](auto shape) {
+    constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = row_threads(G);
     const int64_t grid = std::min<int64_t>(kNormGroupsShort, ceil_div64(n, kThreads / G));
     k_quantize_int<T, G, NV, V><<<(unsigned)grid, kThreads, 0, st>>>(n, f, X, ldx, Q, ldq, S);
   });

@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "agcn_rows.hpp"
+#include "agcn_row_tiles.hpp"
 
 namespace agcn {
 
@@ -280,85 +281,106 @@ __device__ __forceinline__ int64_t token_of(int64_t i) {
          (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)t);
 }
 
-// A row read once and written k times, W bytes a lane at a time (the last piece of a
-// row ends where the row does).
+// A row read once and written k times, U pieces of W bytes a lane at a time (the last piece of
+// a row ends where the row does).
 template <int W>
-struct Bytes {
-  uint8_t b[W];
-};
-template <int W, int G>
+using Bytes = std::conditional_t<W == 16, v4i_any, std::conditional_t<W == 4, uint32_t, uint8_t>>;
+template <int W, int G, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
   const int lane = threadIdx.x % G;
-  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+  for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
     const uint8_t* x = static_cast<const uint8_t*>(a.X) + t * a.ldx;
-    for (int64_t at = lane * W; at < a.f; at += G * W) {
-      const int64_t from = std::min<int64_t>(at, a.f - W);
-      const Bytes<W> v = load_any<Bytes<W>>(x + from), none = {};
+    for (int64_t at = lane * W; at < a.f; at += G * W * U) {
+      Bytes<W> v[U];
+      int64_t from[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        from[u] = std::min<int64_t>(at + u * G * W, a.f - W);
+        v[u] = load_any<Bytes<W>>(x + from[u]);
+      }
       for (int c = 0; c < a.k; ++c) {
         const Slot s(a, t, c);
-        if (s.inside) store_any(static_cast<uint8_t*>(a.out) + s.row * a.ldo + from, s.kept ? v : none);
+        if (!s.inside) continue;
+        uint8_t* to = static_cast<uint8_t*>(a.out) + s.row * a.ldo;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u > 0 && at + u * G * W >= a.f) break;
+          store_row<PAST>(to + from[u], s.kept ? v[u] : Bytes<W>{});
+        }
       }
     }
   }
 }
 
-// out[t] = sum over c of w[t][c] R[place[t][c]], in c's order.
-template <class T, int V, int G>
+// out[t] = sum over c of w[t][c] R[place[t][c]], in c's order, A rows and U pieces of each on
+// their way at a time.
+template <class T, int V, int G, int U, int A, bool PAST>
 __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
-  constexpr int kAtOnce = 4;
   using P = Piece<T, V>;
   const int lane = threadIdx.x % G;
-  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+  for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
-    for (int64_t at = lane * V; at < a.f; at += G * V) {
-      const int64_t from = std::min<int64_t>(at, a.f - V);
-      float sum[V];
+    for (int64_t at = lane * V; at < a.f; at += G * V * U) {
+      int64_t from[U];
+      float sum[U][V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-      for (int c0 = 0; c0 < a.k; c0 += kAtOnce) {
-        P v[kAtOnce];
-        float w[kAtOnce];
-        bool kept[kAtOnce];
+      for (int x = 0; x < U; ++x) {
+        from[x] = std::min<int64_t>(at + x * G * V, a.f - V);
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int e = 0; e < V; ++e) sum[x][e] = 0.0f;
+      }
+      for (int c0 = 0; c0 < a.k; c0 += A) {
+        P v[A][U];
+        float w[A];
+        bool kept[A];
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
           const int c = min(c0 + u, a.k - 1);
           const Slot s(a, t, c);
           kept[u] = s.kept && c0 + u < a.k;
           w[u] = a.w != nullptr ? a.w[t * a.ldw + c] : 1.0f;
-          v[u] = load_any<P>(static_cast<const T*>(a.R) + s.row * a.ldr + from);
+          const T* r = static_cast<const T*>(a.R) + s.row * a.ldr;
+#pragma unroll
+          for (int x = 0; x < U; ++x) v[u][x] = load_row<P, PAST>(r + from[x]);
         }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
+        for (int u = 0; u < A; ++u)
 #pragma unroll
-          for (int e = 0; e < V; ++e) sum[e] = kept[u] ? fmaf(w[u], to_float(v[u].e[e]), sum[e]) : sum[e];
+          for (int x = 0; x < U; ++x)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              sum[x][e] = kept[u] ? fmaf(w[u], to_float(v[u][x].e[e]), sum[x][e]) : sum[x][e];
       }
-      P o;
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.e[e] = (T)sum[e];
-      store_any(static_cast<T*>(a.out) + t * a.ldo + from, o);
+      for (int x = 0; x < U; ++x) {
+        if (x > 0 && at + x * G * V >= a.f) break;
+        P o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.e[e] = (T)sum[x][e];
+        store_row<PAST>(static_cast<T*>(a.out) + t * a.ldo + from[x], o);
+      }
     }
   }
 }
 
 // dR[place[t][c]] = w[t][c] X[t] and dw[t][c] = X[t] . R[place[t][c]], X the gradient of
-// k_combine's sum. A group of lanes has a whole token, kAtOnce slots at a time.
-template <class T, int V, int G>
+// k_combine's sum. A group of lanes has a whole token, A slots and U pieces of each at a time.
+template <class T, int V, int G, int U, int A, bool PAST>
 __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
-  constexpr int kAtOnce = 4;
   using P = Piece<T, V>;
   const int lane = threadIdx.x % G;
-  for (int64_t i = blockIdx.x; i * (256 / G) < a.n; i += gridDim.x) {
+  for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
-    for (int c0 = 0; c0 < a.k; c0 += kAtOnce) {
-      int64_t row[kAtOnce];
-      float w[kAtOnce], dot[kAtOnce];
-      bool kept[kAtOnce], inside[kAtOnce];
+    for (int c0 = 0; c0 < a.k; c0 += A) {
+      int64_t row[A];
+      float w[A], dot[A];
+      bool kept[A], inside[A];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
+      for (int u = 0; u < A; ++u) {
         const int c = min(c0 + u, a.k - 1);
         const Slot s(a, t, c);
         row[u] = s.row;
@@ -367,31 +389,39 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
         w[u] = s.kept ? a.w[t * a.ldw + c] : 0.0f;
         dot[u] = 0.0f;
       }
-      for (int64_t at = lane * V; at < a.f; at += G * V) {
-        const int64_t from = std::min<int64_t>(at, a.f - V);
-        const int shared = (int)(at - from);
-        const P x = load_any<P>(static_cast<const T*>(a.X) + t * a.ldx + from);
-        P r[kAtOnce];
+      for (int64_t at = lane * V; at < a.f; at += G * V * U) {
+        P x[U], r[A][U];
+        int64_t from[U];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) r[u] = load_any<P>(static_cast<const T*>(a.R) + row[u] * a.ldr + from);
+        for (int y = 0; y < U; ++y) {
+          from[y] = std::min<int64_t>(at + y * G * V, a.f - V);
+          x[y] = load_any<P>(static_cast<const T*>(a.X) + t * a.ldx + from[y]);
+        }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          P o;
+        for (int u = 0; u < A; ++u)
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float g = to_float(x.e[e]);
-            o.e[e] = (T)(kept[u] ? w[u] * g : 0.0f);
-            dot[u] = e >= shared ? fmaf(g, to_float(r[u].e[e]), dot[u]) : dot[u];
+          for (int y = 0; y < U; ++y)
+            r[u][y] = load_row<P, PAST>(static_cast<const T*>(a.R) + row[u] * a.ldr + from[y]);
+#pragma unroll
+        for (int y = 0; y < U; ++y) {
+          if (y > 0 && at + y * G * V >= a.f) break;
+          const int shared = (int)(at + y * G * V - from[y]);
+#pragma unroll
+          for (int u = 0; u < A; ++u) {
+            P o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float g = to_float(x[y].e[e]);
+              o.e[e] = (T)(kept[u] ? w[u] * g : 0.0f);
+              dot[u] = e >= shared ? fmaf(g, to_float(r[u][y].e[e]), dot[u]) : dot[u];
+            }
+            if (inside[u]) store_row<PAST>(static_cast<T*>(a.out) + row[u] * a.ldo + from[y], o);
           }
-          if (inside[u]) store_any(static_cast<T*>(a.out) + row[u] * a.ldo + from, o);
         }
       }
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        float d = dot[u];
-        if constexpr (G >= 64) d += __shfl_xor(d, 32);
-        if constexpr (G >= 32) d += __shfl_xor(d, 16);
-        d = sum16(d);
+      for (int u = 0; u < A; ++u) {
+        const float d = lanes_sum<G>(dot[u]);
         if (lane == 0 && c0 + u < a.k) a.dw[t * a.lddw + c0 + u] = kept[u] ? d : 0.0f;
       }
     }
@@ -441,41 +471,85 @@ int sort_typed(SortArgs a, hipStream_t st) {
   return launched("k_group_place launch");
 }
 
-template <class T, int V>
+// Lanes a token (G) and pieces a lane at a time (NV) by a row's pieces, and slots at a time
+// (A) by k. Short rows take few lanes, so that a wave has several tokens' loads on their way: us on
+// one MI355X, 60,000 x 2 slots x 601 float16 45 in 32 lanes of 3 pieces, 48 in 64 of 2, 60 in 256
+// of 1; 200,000 x 128 float32 37 in 16 of 2, 56 in 64 of 1.
+template <bool SHORT, class F>  // SHORT: 8 pieces at most
+void token_shape(int64_t p, F use) {
+  if constexpr (SHORT) {
+    use(Shape<8, 1>{});
+  } else {
+    if (p <= 4) use(Shape<4, 1>{});
+    else if (p <= 8) use(Shape<8, 1>{});
+    else if (p <= 16) use(Shape<16, 1>{});
+    else if (p <= 32) use(Shape<16, 2>{});
+    else if (p <= 48) use(Shape<16, 3>{});
+    else if (p <= 64) use(Shape<16, 4>{});
+    else if (p <= 96) use(Shape<32, 3>{});
+    else if (p <= 128) use(Shape<32, 4>{});
+    else use(Shape<64, 4>{});
+  }
+}
+template <class F>
+void slots_at_once(int32_t k, F use) {
+  if (k <= 1) use(std::integral_constant<int, 1>{});
+  else if (k == 2) use(std::integral_constant<int, 2>{});
+  else if (k % 3 == 0 && k % 4 != 0) use(std::integral_constant<int, 3>{});
+  else use(std::integral_constant<int, 4>{});
+}
+
+template <class T, int V, bool PAST>
 int combine_pieces(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = ceil_div64(a.f, V);
-  if (pieces <= 4) k_combine<T, V, 4><<<row_grid<4>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 16) k_combine<T, V, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 64) k_combine<T, V, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else k_combine<T, V, 256><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  slots_at_once(a.k, [&](auto at_once) {
+    constexpr int A = decltype(at_once)::value;
+    // Rows over 4 KB: the lanes of four waves, two pieces each.
+    if (V > 1 && pieces > 256) {
+      k_combine<T, V, 256, 2, A, PAST><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+      return;
+    }
+    token_shape<V == 1>(pieces, [&](auto shape) {
+      constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
+      k_combine<T, V, G, U, A, PAST><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+    });
+  });
   return launched("k_combine launch");
 }
-template <class T, int V>
+template <class T, int V, bool PAST>
 int combine_grad_pieces(const RowArgs& a, hipStream_t st) {
-  if (ceil_div64(a.f, V) <= 16) k_combine_grad<T, V, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
-  else k_combine_grad<T, V, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  slots_at_once(a.k, [&](auto at_once) {
+    constexpr int A = decltype(at_once)::value;
+    token_shape<V == 1>(ceil_div64(a.f, V), [&](auto shape) {
+      constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
+      k_combine_grad<T, V, G, U, A, PAST><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+    });
+  });
   return launched("k_combine_grad launch");
 }
 
 template <class T>
 int combine_typed(const RowArgs& a, bool grad, hipStream_t st) {
   constexpr int V = kPiece<T>;
-  if (grad) return a.f < V ? combine_grad_pieces<T, 1>(a, st) : combine_grad_pieces<T, V>(a, st);
-  return a.f < V ? combine_pieces<T, 1>(a, st) : combine_pieces<T, V>(a, st);
+  if (a.f < V) return grad ? combine_grad_pieces<T, 1, false>(a, st) : combine_pieces<T, 1, false>(a, st);
+  const bool past = on_lines(a.R, a.ldr, sizeof(T)) && on_lines(a.out, a.ldo, sizeof(T));
+  if (grad) return past ? combine_grad_pieces<T, V, true>(a, st) : combine_grad_pieces<T, V, false>(a, st);
+  return past ? combine_pieces<T, V, true>(a, st) : combine_pieces<T, V, false>(a, st);
 }
 int combine_any(const RowArgs& a, int32_t dtype, bool grad, hipStream_t st) {
   if (dtype == AGCN_FLOAT) return combine_typed<float>(a, grad, st);
   return dtype == AGCN_BFLOAT ? combine_typed<bf16_t>(a, grad, st) : combine_typed<f16_t>(a, grad, st);
 }
 
-template <int W>
+template <int W, bool PAST>
 int dispatch_pieces(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = ceil_div64(a.f, W);
-  if (pieces <= 1) k_dispatch<W, 1><<<row_grid<1>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 4) k_dispatch<W, 4><<<row_grid<4>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 16) k_dispatch<W, 16><<<row_grid<16>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 64) k_dispatch<W, 64><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else k_dispatch<W, 256><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  if (pieces <= 1) k_dispatch<W, 1, 1, PAST><<<row_grid<1>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 4) k_dispatch<W, 4, 1, PAST><<<row_grid<4>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 16 || W < 16) k_dispatch<W, 16, 1, PAST><<<row_grid<16>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 64) k_dispatch<W, 64, 1, PAST><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 128) k_dispatch<W, 64, 2, PAST><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else k_dispatch<W, 256, 2, PAST><<<row_grid<256>(a.n), 256, 0, st>>>(a);
   return launched("k_dispatch launch");
 }
 
@@ -498,8 +572,8 @@ int run_dispatch(int64_t n, int32_t k, int64_t bytes, const void* X, int64_t ldx
   if (n == 0 || k == 0 || bytes == 0) return AGCN_OK;
   RowArgs a{};
   a.n = n, a.f = bytes, a.k = k, a.place = place, a.ldp = ldp, a.X = X, a.ldx = ldx, a.out = Y, a.ldo = ldy;
-  if (bytes >= 16) return dispatch_pieces<16>(a, st);
-  return bytes >= 4 ? dispatch_pieces<4>(a, st) : dispatch_pieces<1>(a, st);
+  if (bytes >= 16) return on_lines(Y, ldy, 1) ? dispatch_pieces<16, true>(a, st) : dispatch_pieces<16, false>(a, st);
+  return bytes >= 4 ? dispatch_pieces<4, false>(a, st) : dispatch_pieces<1, false>(a, st);
 }
 
 int run_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* R, int64_t ldr, const int32_t* place,
