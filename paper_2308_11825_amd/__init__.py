@@ -6,8 +6,10 @@ low-level functions carry the C names of ``include/agcn.h``; ``Plan`` wraps
 them for torch tensors.
 
 The library must have been built (``python -m paper_2308_11825_amd.build``);
-there is no fallback of any kind: if ``libagcn.so`` is missing, importing the
-functions that need it raises.
+there is no fallback of any kind: if ``libagcn.so`` is missing, the functions that
+need it raise. The functions of the routed layer's operators are compiled
+(``_binding.so``, built with the library): their calls on a few rows take as long
+as their marshalling does.
 """
 from __future__ import annotations
 
@@ -835,36 +837,44 @@ def grouped_linear(Q, S, WQ, WS, offsets, dtype=None, act=None, out=None, stream
 # A matrix in 8-bit integers is a pair of tensors: the values Q (torch.int8) and a float32
 # scale S for each row, or for each output of a weight. It stands for Q times its scales.
 
-def _vector(name, t, device, shape, dtype):
-    """Checks `t`, a contiguous vector (or stacked ones, contiguous each) of this shape."""
-    if not isinstance(t, _torch.Tensor) or t.device != device:
-        raise TypeError(f"{name} must be a tensor on {device}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must have dtype {dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}")
-    if shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name} must be contiguous")
+_native = None  # the compiled binding of these functions and of those below
+_NATIVE = ["layer_norm", "layer_norm_workspace_size", "layer_norm_backward",
+           "sort_groups_workspace_size", "sort_groups", "dispatch", "combine", "combine_backward",
+           "quantize_rows_int", "int_linear", "grouped_int_linear", "last_error"]
+
+
+def _call_native(name, stream, *args):
+    """`name` of the compiled binding. It allocates on the current stream and runs there: the
+    caller's, if one is given, and then torch's allocator must not reuse the tensors' memory
+    before its work."""
+    native = _native or _load_native()
+    if stream is None:
+        return getattr(native, name)(*args)
+    with _torch.cuda.stream(stream):
+        results = getattr(native, name)(*args)
+    for t in args:
+        for t in t if isinstance(t, tuple) else (t,):
+            if isinstance(t, _torch.Tensor):
+                t.record_stream(stream)
+    return results
+
+
+def _load_native():
+    global _native
+    lib = load_library()
+    if _torch is None:
+        _load_torch()
+    from . import _binding
+    _binding.init(AgcnError, [ctypes.cast(getattr(lib, "agcn_" + n), _vp).value for n in _NATIVE])
+    _native = _binding
+    return _native
 
 
 def quantize_int(X, out=None, stream=None):
     """The rows of X (n, f) in 8-bit integers: (Q, S), Q (n, f) int8 and S (n,) float32, a
     127th of the row's largest value. X: float32, bfloat16 or float16 CUDA tensor; out: such a
     pair to write to."""
-    (n, f), device = _first("X", X, 2)
-    dtype = X.dtype
-    code, ldx = _dtype_code("X", dtype), _matrix("X", X, device, X.shape, dtype)
-    if out is None:
-        Q, ldq = _new_rows(X, stream, (n,), f, _torch.int8)
-        S = _new(X, stream, (n,), _torch.float32)
-    else:
-        Q, S = out
-        ldq = _matrix("out[0]", Q, device, (n, f), _torch.int8)
-        _vector("out[1]", S, device, (n,), _torch.float32)
-    st = _on_stream(device, stream, (X, Q, S))
-    _call(device, agcn_quantize_rows_int, n, f, code, X.data_ptr(), ldx, Q.data_ptr(), ldq,
-          S.data_ptr(), st)
-    return Q, S
+    return _call_native("quantize_int", stream, X, out)
 
 
 def quantize_weight_int(W, stream=None):
@@ -885,35 +895,10 @@ def quantize_weight_int(W, stream=None):
 
 
 def _int_product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
-    shape, device = _first("Q", Q, 2)
-    w_shape, _ = _first("WQ", WQ, 2 if offsets is None else 3, weight=True)
-    n, fin = shape
-    fout, lead = w_shape[-2], w_shape[:-2]
-    ldq = _matrix("Q", Q, device, shape, _torch.int8)
-    _vector("S", S, device, (n,), _torch.float32)
-    ldwq = _matrix("WQ", WQ, device, (*lead, fout, fin), _torch.int8)
-    _vector("WS", WS, device, (*lead, fout), _torch.float32)
     epilogue = _EPILOGUES.get(act)
     if epilogue is None:
         raise ValueError("act must be None, 'none' or 'relu'")
-    if out is None:
-        dtype = _torch.float32 if dtype is None else dtype
-        code = _dtype_code("the result", dtype)
-        out, ldy = _new(Q, stream, (n, fout), dtype), fout
-    else:
-        code = _dtype_code("out", getattr(out, "dtype", None))
-        ldy = _matrix("out", out, device, (n, fout), out.dtype if dtype is None else dtype)
-    st = _on_stream(device, stream, (Q, S, WQ, WS, offsets, out))
-    if offsets is None:
-        _call(device, agcn_int_linear, n, fin, fout, Q.data_ptr(), ldq, S.data_ptr(), WQ.data_ptr(),
-              ldwq, WS.data_ptr(), code, out.data_ptr(), ldy, st, epilogue)
-        return out
-    groups = lead[0]
-    _vector("offsets", offsets, device, (groups + 1,), _torch.int32)
-    _call(device, agcn_grouped_int_linear, n, fin, fout, groups, Q.data_ptr(), ldq, S.data_ptr(),
-          WQ.data_ptr(), ldwq, WQ.stride(0), WS.data_ptr(), WS.stride(0), offsets.data_ptr(), code,
-          out.data_ptr(), ldy, st, epilogue)
-    return out
+    return _call_native("int_product", stream, Q, S, WQ, WS, offsets, dtype, epilogue, out)
 
 
 def int_linear(Q, S, WQ, WS, dtype=None, act=None, out=None, stream=None):
@@ -942,52 +927,7 @@ def layer_norm(X, weight, bias=None, residual=None, eps=1e-5, stats=False, hidde
     X, residual, h and y are (n, f) of one type (float32, bfloat16 or float16), weight and bias
     (f,) both of that type or float32. hidden: where h is written (X or residual itself will
     do); out: where y is."""
-    (n, f), device = _first("X", X, 2)
-    dtype, shape = X.dtype, X.shape
-    code, ldx = _dtype_code("X", dtype), _matrix("X", X, device, shape, dtype)
-    p_code = _parameter("weight", weight, device, f, dtype)
-    b = None
-    if bias is not None:
-        _vector("bias", bias, device, (f,), weight.dtype)
-        b = bias.data_ptr()
-    r = h = s = None
-    ldr = ldh = 0
-    if residual is not None:
-        ldr = _matrix("residual", residual, device, shape, dtype)
-        r = residual.data_ptr()
-        if hidden is None:
-            hidden, ldh = _new(X, stream, shape, dtype), f
-        else:
-            ldh = _matrix("hidden", hidden, device, shape, dtype)
-        h = hidden.data_ptr()
-    elif hidden is not None:
-        raise ValueError("hidden needs a residual: without one h is X")
-    if out is None:
-        out, ldy = _new(X, stream, shape, dtype), f
-    else:
-        ldy = _matrix("out", out, device, shape, dtype)
-    if stats:
-        if f == 0:
-            raise ValueError("rows of no columns have no statistics")
-        stats = _new(X, stream, (n, 2), _torch.float32)
-        s = stats.data_ptr()
-    st = _on_stream(device, stream, (X, weight, bias, residual, hidden, out))
-    _call(device, agcn_layer_norm, n, f, code, X.data_ptr(), ldx, r, ldr, h, ldh, weight.data_ptr(),
-          b, p_code, eps, out.data_ptr(), ldy, s, 2, st)
-    results = (out,) if residual is None else (out, hidden)
-    if stats is not False:
-        results += (stats,)
-    return results if len(results) > 1 else out
-
-
-def _parameter(name, t, device, f, dtype):
-    """The type code of a norm's parameter, (f,) float32 or of the rows' type."""
-    if not isinstance(t, _torch.Tensor) or t.device != device:
-        raise TypeError(f"{name} must be a tensor on X's device")
-    if t.dtype is not dtype and t.dtype is not _torch.float32:
-        raise TypeError(f"{name} must be float32 or of X's type")
-    _vector(name, t, device, (f,), t.dtype)
-    return _DTYPES[t.dtype]
+    return _call_native("layer_norm", stream, X, weight, bias, residual, eps, stats, hidden, out)
 
 
 def layer_norm_backward(grad, H, stats, weight, bias=True, grad_hidden=None, out=None, stream=None):
@@ -995,30 +935,7 @@ def layer_norm_backward(grad, H, stats, weight, bias=True, grad_hidden=None, out
     where there was no residual); stats: as ``layer_norm`` gave them; grad_hidden: the gradient
     of h from elsewhere, added to dX, which is that of X and of the residual; bias=False: dbias
     is None; out: where dX is written. dweight and dbias have weight's type."""
-    (n, f), device = _first("grad", grad, 2)
-    dtype, shape = grad.dtype, grad.shape
-    code, lddy = _dtype_code("grad", dtype), _matrix("grad", grad, device, shape, dtype)
-    ldh = _matrix("H", H, device, shape, dtype)
-    lds = _matrix("stats", stats, device, (n, 2), _torch.float32)
-    p_code = _parameter("weight", weight, device, f, dtype)
-    d = None
-    ldd = 0
-    if grad_hidden is not None:
-        ldd = _matrix("grad_hidden", grad_hidden, device, shape, dtype)
-        d = grad_hidden.data_ptr()
-    if out is None:
-        out, lddx = _new(grad, stream, shape, dtype), f
-    else:
-        lddx = _matrix("out", out, device, shape, dtype)
-    dw = _new(grad, stream, (f,), weight.dtype)
-    db = _new(grad, stream, (f,), weight.dtype) if bias else None
-    nb = agcn_layer_norm_workspace_size(n, f, code)
-    ws = _new(grad, stream, (nb // 4,), _torch.float32) if nb else None
-    st = _on_stream(device, stream, (grad, H, stats, weight, grad_hidden, out))
-    _call(device, agcn_layer_norm_backward, n, f, code, grad.data_ptr(), lddy, H.data_ptr(), ldh, d,
-          ldd, stats.data_ptr(), lds, weight.data_ptr(), p_code, out.data_ptr(), lddx, dw.data_ptr(),
-          db.data_ptr() if bias else None, ws.data_ptr() if nb else None, st)
-    return out, dw, db
+    return _call_native("layer_norm_backward", stream, grad, H, stats, weight, bias, grad_hidden, out)
 
 
 # ---- rows sent to groups and back ----
@@ -1029,101 +946,25 @@ def sort_groups(ids, groups, out=None, stream=None):
     group of the ids; offsets (groups + 1,): group e has the places offsets[e] to
     offsets[e + 1] - 1, as ``grouped_linear`` takes them. Ids outside [0, groups) get the
     places from offsets[groups] on, written as -1 - place. out: such a pair to write to."""
-    (n, k), device = _first("ids", ids, 2)
-    if ids.dtype is not _torch.int32 and ids.dtype is not _torch.int64:
-        raise TypeError("ids must have dtype int32 or int64")
-    if not 0 <= groups <= _MOST_INT32:
-        raise ValueError("groups must be from 0 to 2^31 - 1")
-    groups = int(groups)
-    ldi = _matrix("ids", ids, device, (n, k), ids.dtype)
-    if out is None:
-        offsets = _new(ids, stream, (groups + 1,), _torch.int32)
-        place, ldp = _new(ids, stream, (n, k), _torch.int32), k
-    else:
-        offsets, place = out
-        _vector("out[0]", offsets, device, (groups + 1,), _torch.int32)
-        ldp = _matrix("out[1]", place, device, (n, k), _torch.int32)
-    nb = agcn_sort_groups_workspace_size(n, k, groups)
-    ws = _new(ids, stream, (nb // 4,), _torch.int32) if nb else None
-    st = _on_stream(device, stream, (ids, offsets, place))
-    _call(device, agcn_sort_groups, n, k, groups, ids.data_ptr(), ids.element_size(), ldi,
-          offsets.data_ptr(), place.data_ptr(), ldp, ws.data_ptr() if nb else None, st)
-    return offsets, place
+    return _call_native("sort_groups", stream, ids, groups, out)
 
 
 def dispatch(X, place, out=None, stream=None):
     """The rows of X (n, f), of any type, in group order: (n * k, f) with row place[t][c] = X[t],
     and rows of ids without a group 0. Its gradient is ``combine`` of the rows' without
     weights."""
-    (n, f), device = _first("X", X, 2)
-    k = place.shape[1] if getattr(place, "ndim", 0) == 2 else 0
-    dtype, size = X.dtype, X.element_size()
-    ldx = _matrix("X", X, device, (n, f), dtype)
-    ldp = _matrix("place", place, device, (n, k), _torch.int32)
-    if out is None:
-        if size == 1:
-            out, ldy = _new_rows(X, stream, (n * k,), f, dtype)
-        else:
-            out, ldy = _new(X, stream, (n * k, f), dtype), f
-    else:
-        ldy = _matrix("out", out, device, (n * k, f), dtype)
-    st = _on_stream(device, stream, (X, place, out))
-    _call(device, agcn_dispatch, n, k, f * size, X.data_ptr(), ldx * size, place.data_ptr(), ldp,
-          out.data_ptr(), ldy * size, st)
-    return out
+    return _call_native("dispatch", stream, X, place, out)
 
 
 def combine(R, place, weights=None, out=None, stream=None):
     """(n, f) with row t the sum over c of weights[t][c] R[place[t][c]], ids without a group left
     out: R (n * k, f) float32, bfloat16 or float16 rows in group order, place (n, k) as
     ``sort_groups`` gives it, weights (n, k) float32 or None (all 1). Added in 32 bits."""
-    (rows, f), device = _first("R", R, 2)
-    dtype = R.dtype
-    code = _dtype_code("R", dtype)
-    n, k, ldp = _places(place, device, rows)
-    ldr = _matrix("R", R, device, (rows, f), dtype)
-    w, ldw = None, k
-    if weights is not None:
-        ldw = _matrix("weights", weights, device, (n, k), _torch.float32)
-        w = weights.data_ptr()
-    if out is None:
-        out, ldy = _new(R, stream, (n, f), dtype), f
-    else:
-        ldy = _matrix("out", out, device, (n, f), dtype)
-    st = _on_stream(device, stream, (R, place, weights, out))
-    _call(device, agcn_combine, n, k, f, code, R.data_ptr(), ldr, place.data_ptr(), ldp, w, ldw,
-          out.data_ptr(), ldy, st)
-    return out
-
-
-def _places(place, device, rows):
-    """(n, k) and the row stride of the places of `rows` rows."""
-    if not isinstance(place, _torch.Tensor) or place.dim() != 2:
-        raise TypeError("place must be an (n, k) int32 CUDA tensor")
-    n, k = place.shape
-    ldp = _matrix("place", place, device, (n, k), _torch.int32)
-    if n * k != rows:
-        raise ValueError("place must name as many rows as there are")
-    return n, k, ldp
+    return _call_native("combine", stream, R, place, weights, out)
 
 
 def combine_backward(grad, R, place, weights, out=None, stream=None):
     """Gradients of ``combine`` with weights from grad (n, f), that of its result: (dR, dweights),
     dR (n * k, f) of R's type and dweights (n, k) float32, 0 for ids without a group. out: where dR
     is written. (Without weights dR is ``dispatch`` of grad.)"""
-    (rows, f), device = _first("R", R, 2)
-    dtype = R.dtype
-    code = _dtype_code("R", dtype)
-    n, k, ldp = _places(place, device, rows)
-    ldr = _matrix("R", R, device, (rows, f), dtype)
-    ldg = _matrix("grad", grad, device, (n, f), dtype)
-    ldw = _matrix("weights", weights, device, (n, k), _torch.float32)
-    if out is None:
-        out, ldo = _new(R, stream, (rows, f), dtype), f
-    else:
-        ldo = _matrix("out", out, device, (rows, f), dtype)
-    dw = _new(R, stream, (n, k), _torch.float32)
-    st = _on_stream(device, stream, (grad, R, place, weights, out))
-    _call(device, agcn_combine_backward, n, k, f, code, grad.data_ptr(), ldg, R.data_ptr(), ldr,
-          place.data_ptr(), ldp, weights.data_ptr(), ldw, out.data_ptr(), ldo, dw.data_ptr(), k, st)
-    return out, dw
+    return _call_native("combine_backward", stream, grad, R, place, weights, out)
