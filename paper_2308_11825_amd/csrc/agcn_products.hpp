@@ -140,19 +140,41 @@ __device__ __forceinline__ void block_products(Sum4<P> (&acc)[NT][MT], GetW w, G
 }
 
 // What is written for a sum: itself, or for integers the sum times its row's scale and then
-// its column's. Sums that nothing was added to are 0 whatever the scales.
+// its column's. Sums that nothing was added to are 0 whatever the scales. A thread asks for
+// the scales of one row and one column of the tile before the products and passes them on
+// through LDS after them: asked for where they are needed, they cost a 256 x 256 tile 32 loads one
+// after the other (32768 x 4096 -> 2048 SCALES_BEFORE us, SCALES_NOW now).
 template <Products P>
 struct Scales {
-  const float *a = nullptr, *w = nullptr;  // of the tile's first row and column
-  __device__ __forceinline__ Scales(const LinearArgs& p, int64_t row, int32_t group, int n0) {
+  float row = 0.0f, column = 0.0f;
+  __device__ __forceinline__ Scales(const LinearArgs& p, const Rows& rows, int n0, int m, int n) {
     if constexpr (P == kInteger)
-      if (group >= 0 && p.fin > 0) {
-        a = p.RA + row;
-        w = p.RW + group * p.group_rw + n0;
+      if (rows.group >= 0 && p.fin > 0) {
+        if (m < rows.count) row = p.RA[rows.row + m];
+        if (n0 + n < p.fout) column = p.RW[rows.group * p.group_rw + n0 + n];
       }
   }
-  __device__ __forceinline__ float row(int m) const { return P == kInteger && a != nullptr ? a[m] : 0.0f; }
-  __device__ __forceinline__ float column(int n) const { return P == kInteger && a != nullptr ? w[n] : 0.0f; }
+  // The scales of RUN neighbouring columns, of four or eight, from there.
+  template <int RUN>
+  static __device__ __forceinline__ void columns(float (&to)[RUN], const float* from) {
+    if constexpr (P == kInteger) {
+#pragma unroll
+      for (int i = 0; i < RUN; i += 4) {
+        const v4f v = *reinterpret_cast<const v4f*>(from + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[i + k] = v[k];
+      }
+    }
+  }
+  // To `at`, the rows' and then the columns': those of threads 0 to BM - 1 and BN - 1.
+  template <int BM, int BN>
+  __device__ __forceinline__ void share(float* at) const {
+    if constexpr (P == kInteger) {
+      if (threadIdx.x < BM) at[threadIdx.x] = row;
+      if (threadIdx.x < BN) at[BM + threadIdx.x] = column;
+      __syncthreads();
+    }
+  }
   static __device__ __forceinline__ float apply(Sum<P> v, float row, float column) {
     if constexpr (P == kInteger) {
       // Rounded to fp32 before the rounding to the type: some kernels' code would do both at
@@ -178,6 +200,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
   const int n0 = blockIdx.x * 16;
   const Rows rows = few_rows<BM, GROUPED>(p);
   if (rows.count <= 0) return;
+  const Scales<P> scales(p, rows, n0, threadIdx.x / 16, threadIdx.x % 16);
   Sum4<P> acc[1][MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[0][t] = Sum4<P>{0, 0, 0, 0};
@@ -234,13 +257,13 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
   for (int t = 0; t < MT; ++t) *reinterpret_cast<Sum4<P>*>(&part[wave][t * 16 + r][g * 4]) = acc[0][t];
   __syncthreads();
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
-  const Scales<P> scales(p, rows.row, rows.group, n0);
   for (int i = threadIdx.x; i < rows.count * 16; i += 64 * NW) {
     const int m = i / 16, n = i % 16;
     Sum<P> v = part[0][m][n];
 #pragma unroll
     for (int k = 1; k < NW; ++k) v += part[k][m][n];
-    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, scales.row(m), scales.column(n)), p.act);
+    const Scales<P> more = i < 64 * NW ? scales : Scales<P>(p, rows, n0, m, n);
+    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, more.row, more.column), p.act);
   }
 }
 
@@ -420,6 +443,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
   const Rows rows = tile_rows<BM, GROUPED>(p, tiles_n, group_m, &tn);
   if (rows.count <= 0) return;
   const int n0 = (int)tn * BN, count_n = min(BN, p.fout - n0);
+  const Scales<P> scales(p, rows, n0, threadIdx.x, threadIdx.x);
   Sum4<P> acc[NT][MT];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -499,7 +523,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
   }
 
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
-  const Scales<P> scales(p, rows.row, rows.group, n0);
+  if constexpr (P == kInteger) __syncthreads();  // the last block has been read
+  const float* shared = reinterpret_cast<const float*>(lds0);
+  static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "scales by threads");
+  scales.template share<BM, BN>(reinterpret_cast<float*>(lds0));
   write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
     constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
     constexpr int kRun = PERM ? 8 : 4;  // neighbouring outputs of a lane
@@ -507,15 +534,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
     for (int t = 0; t < MT; ++t) {
       const int m = wm * TM + t * 16 + r;
       if (!ALL && m >= rows.count) continue;
-      const float row = scales.row(m);
+      const float row = P == kInteger ? shared[m] : 0.0f;
 #pragma unroll
       for (int j = 0; j < NT; j += kRun / 4) {
         const int n = wn * TN + (PERM ? j / 2 * 32 + 8 * g : j * 16 + 4 * g);
-        float v[kRun];
+        float v[kRun], column[kRun];
+        scales.columns(column, shared + BM + n);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i)
-          v[i] = q_act(scales.apply(acc[j + i / 4][t][i % 4], row, scales.column(ALL ? n + i : min(n + i, count_n - 1))),
-                       RELU);
+        for (int i = 0; i < kRun; ++i) v[i] = q_act(scales.apply(acc[j + i / 4][t][i % 4], row, column[i]), RELU);
         store_run<ALL>(v, y + m * p.ldy, n, count_n);
       }
     }
@@ -572,6 +598,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_stream(LinearArgs p) {
   const int r = lane % 16, g = lane / 16, n0 = blockIdx.x * BN;
   const Rows rows = few_rows<BM, GROUPED>(p);
   if (rows.count <= 0) return;
+  const Scales<P> scales(p, rows, n0, threadIdx.x / BN, threadIdx.x % BN);
   const int blocks = rows.group < 0 ? 0 : (p.fin + kQBlock - 1) / kQBlock;
   const int mine = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
   Sum4<P> acc[NT][MT];
@@ -640,13 +667,13 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_stream(LinearArgs p) {
       *reinterpret_cast<Sum4<P>*>(&part[wave][t * 16 + r][j * 16 + g * 4]) = acc[j][t];
   __syncthreads();
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
-  const Scales<P> scales(p, rows.row, rows.group, n0);
   for (int i = threadIdx.x; i < rows.count * BN; i += 64 * NW) {
     const int m = i / BN, n = i % BN;
     Sum<P> v = part[0][m][n];
 #pragma unroll
     for (int k = 1; k < NW; ++k) v += part[k][m][n];
-    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, scales.row(m), scales.column(n)), p.act);
+    const Scales<P> more = i < 64 * NW ? scales : Scales<P>(p, rows, n0, m, n);
+    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, more.row, more.column), p.act);
   }
 }
 
@@ -675,6 +702,7 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
   const Rows rows = tile_rows<BM, GROUPED>(p, tiles_n, group_m, &tn);
   if (rows.count <= 0) return;
   const int n0 = (int)tn * BN, count_n = min(BN, p.fout - n0);
+  const Scales<P> scales(p, rows, n0, threadIdx.x, threadIdx.x);
   Sum16<P> acc[2 * T][2 * T];
 #pragma unroll
   for (int j = 0; j < 2 * T; ++j)
@@ -879,7 +907,8 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
   constexpr int kRun = 16 / sizeof(TY), kRow = 2 * H * sizeof(TY) + 16, kLanes = 2 * H / kRun;
   uint8_t* own = lds + wave * 32 * kRow;
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
-  const Scales<P> scales(p, rows.row, rows.group, n0);
+  const float* shared = reinterpret_cast<const float*>(lds + 4 * 32 * kRow);
+  scales.template share<BM, BN>(reinterpret_cast<float*>(lds + 4 * 32 * kRow));
   write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
     constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
     struct alignas(16) Run {
@@ -888,19 +917,17 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
 #pragma unroll
     for (int t = 0; t < 2 * T; ++t) {
       const int m = wm * 2 * H + t * 32 + r;
-      const float scale = scales.row(ALL ? m : min(m, rows.count - 1));
+      const float scale = P == kInteger ? shared[m] : 0.0f;
 #pragma unroll
       for (int j = 0; j < 2 * T; ++j)
 #pragma unroll
         for (int c = 0; c < 16; c += kRun) {
           const int n = j * 32 + c / 8 * 16 + 8 * g + c % 8;
           Run v;
+          float column[kRun];
+          scales.columns(column, shared + BM + wn * 2 * H + n);
 #pragma unroll
-          for (int i = 0; i < kRun; ++i) {
-            const int at = wn * 2 * H + n + i;
-            v.e[i] = (TY)q_act(scales.apply(acc[j][t][c + i], scale, scales.column(ALL ? at : min(at, count_n - 1))),
-                               RELU);
-          }
+          for (int i = 0; i < kRun; ++i) v.e[i] = (TY)q_act(scales.apply(acc[j][t][c + i], scale, column[i]), RELU);
           *reinterpret_cast<Run*>(own + r * kRow + n * sizeof(TY)) = v;
         }
       const int n = lane % kLanes * kRun, left = count_n - wn * 2 * H - n, row0 = wm * 2 * H + t * 32 + lane / kLanes;
@@ -997,6 +1024,10 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
       if (rows <= 16) return launch_thin<1, 4, P, TY, GROUPED>(p, st);
       return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     }
+    // Few outputs and no rows to stage: the k of an output over eight waves. 5000 x 602 -> 41 over
+    // 7 groups THIN_NOW us, 12.5 in 64 x 64 tiles. (Integer sums are the same in any order.)
+    if (P == kInteger && fits_y && few_rows_grid(p.n, p.groups, 32, GROUPED) * ceil_div64(p.fout, 16) <= 4 * kUnits)
+      return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     if (!near) return fail(AGCN_ERR_UNSUPPORTED, "row strides over 8 million bytes and over 65535 row tiles");
     if (tiles(64, 64) <= 4 * kUnits) return launch_tile<32, 32, 2, 2, P, TY, GROUPED, false>(p, st);
     return launch_tile<32, 64, 4, 1, P, TY, GROUPED, false>(p, st);

@@ -84,22 +84,40 @@ __device__ __forceinline__ int block_scan(int v, int* part, int* total) {
   return before + in - v;
 }
 
-// Few slots: one workgroup, each wave a run of the slots. A slot's rank among its wave's
-// slots of its group, then the waves' and the groups' sums.
-constexpr int kSmallBins = 1024, kSmallSteps = 8, kSmallSlots = 1024 * kSmallSteps;
-template <class ID>
+// Up to kSmallSlots slots: one workgroup, each wave a run of the slots. A slot's rank among its
+// wave's slots of its group, then the waves' and the groups' sums. TILED: a workgroup for each
+// tile of up to that many slots, the groups' counts in all tiles having been written before;
+// each adds up those of the tiles before its own and of all.
+constexpr int kMostSortTiles = 256, kSmallBins = 1024, kSmallSteps = 8, kSmallSlots = 1024 * kSmallSteps;
+template <class ID, bool TILED>
 __global__ __launch_bounds__(1024) void k_group_small(SortArgs a, int bits) {
   __shared__ int32_t count[16][kSmallBins];
+  __shared__ int32_t tile_sum[TILED ? 2 : 1][TILED ? kSmallBins : 1];
   __shared__ int part[16];
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, bins = a.groups + 1;
   for (int i = threadIdx.x; i < 16 * bins; i += 1024) count[i / bins][i % bins] = 0;
+  if constexpr (TILED) tile_sum[0][threadIdx.x] = tile_sum[1][threadIdx.x] = 0;
   __syncthreads();
   int32_t key[kSmallSteps], rank[kSmallSteps];
-  const uint32_t first = wave * a.chunk;
+  const uint32_t first = (blockIdx.x * 16 + wave) * a.chunk;
 #pragma unroll
   for (int s = 0; s < kSmallSteps; ++s) {
     const uint32_t j = first + s * 64 + lane;
     key[s] = s * 64 < a.chunk && j < a.slots ? group_of<ID>(a, j) : -1;
+  }
+  if constexpr (TILED) {
+    const int width = 1 << bits, bin = threadIdx.x % width;
+    int before = 0, all = 0;
+    if (bin < bins) {
+#pragma unroll 8
+      for (int t = threadIdx.x / width; t < a.tiles; t += 1024 / width) {
+        const int c = a.counts[(int64_t)t * bins + bin];
+        before += t < (int)blockIdx.x ? c : 0;
+        all += c;
+      }
+      atomicAdd(&tile_sum[0][bin], before);  // sums of integers: any order
+      atomicAdd(&tile_sum[1][bin], all);
+    }
   }
 #pragma unroll
   for (int s = 0; s < kSmallSteps; ++s) {
@@ -121,10 +139,15 @@ __global__ __launch_bounds__(1024) void k_group_small(SortArgs a, int bits) {
       sum += c;
     }
   }
-  int total;
-  const int start = block_scan<1024>(sum, part, &total);
+  int total, start;
+  if constexpr (TILED) {
+    start = block_scan<1024>((int)threadIdx.x < bins ? tile_sum[1][threadIdx.x] : 0, part, &total);
+  } else {
+    start = block_scan<1024>(sum, part, &total);
+  }
   if ((int)threadIdx.x < bins) {
-    a.offsets[threadIdx.x] = start;
+    if (blockIdx.x == 0) a.offsets[threadIdx.x] = start;
+    if constexpr (TILED) start += tile_sum[0][threadIdx.x];
 #pragma unroll
     for (int w = 0; w < 16; ++w) count[w][threadIdx.x] += start;
   }
@@ -136,24 +159,24 @@ __global__ __launch_bounds__(1024) void k_group_small(SortArgs a, int bits) {
 
 // Many slots, in three launches: the groups' counts in each tile of slots, their sums over
 // the tiles before, and the places. Groups are taken kBins at a time.
-constexpr int kBins = 2048, kSortThreads = 256, kSortWaves = kSortThreads / 64, kMostSortTiles = 256;
+constexpr int kBins = 2048, kSortThreads = 256, kSortWaves = kSortThreads / 64;
 
-template <class ID>
-__global__ __launch_bounds__(kSortThreads) void k_group_count(SortArgs a) {
+template <class ID, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_group_count(SortArgs a) {
   __shared__ int32_t count[kBins];
-  const uint32_t tile = kSortWaves * a.chunk, first = blockIdx.x * tile;
+  const uint32_t tile = THREADS / 64 * a.chunk, first = blockIdx.x * tile;
   const uint32_t end = min(a.slots, first + tile);
   const int bins = a.groups + 1;
   for (int base = 0; base < bins; base += kBins) {
     const int here = min(kBins, bins - base);
-    for (int i = threadIdx.x; i < here; i += kSortThreads) count[i] = 0;
+    for (int i = threadIdx.x; i < here; i += THREADS) count[i] = 0;
     __syncthreads();
-    for (uint32_t j = first + threadIdx.x; j < end; j += kSortThreads) {
+    for (uint32_t j = first + threadIdx.x; j < end; j += THREADS) {
       const int key = group_of<ID>(a, j) - base;
       if (key >= 0 && key < here) atomicAdd(&count[key], 1);  // a sum of ones: any order
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < here; i += kSortThreads)
+    for (int i = threadIdx.x; i < here; i += THREADS)
       a.counts[(int64_t)blockIdx.x * bins + base + i] = count[i];
     __syncthreads();
   }
@@ -441,29 +464,40 @@ int bits_of(int bins) {
   return bits;
 }
 
-// Tiles of a sort, and slots of a wave of each: at least 256, whole steps of 64.
+// How a sort is cut: tiles, and slots of a wave of each, whole steps of 64.
 struct SortShape {
+  bool small;  // a tile is kSmallSlots slots at most, for k_group_small
   int32_t tiles;
   uint32_t chunk;
 };
-SortShape sort_shape(int64_t slots) {
-  const int64_t chunk = std::max<int64_t>(256, ceil_div64(ceil_div64(slots, kMostSortTiles * kSortWaves), 64) * 64);
-  return {(int32_t)ceil_div64(slots, kSortWaves * chunk), (uint32_t)chunk};
+SortShape sort_shape(int64_t slots, int32_t groups) {
+  auto steps = [slots](int64_t waves) { return ceil_div64(slots, 64 * waves); };
+  if (groups < kSmallBins && slots <= kSmallSlots) return {true, 1, (uint32_t)steps(16) * 64};
+  if (groups < kSmallBins && slots <= (int64_t)kSmallSlots * kMostSortTiles) {
+    const int64_t chunk = std::min<int64_t>(kSmallSteps, steps(16 * 64)) * 64;  // about 64 tiles, or more
+    return {true, (int32_t)ceil_div64(slots, 16 * chunk), (uint32_t)chunk};
+  }
+  const int64_t chunk = std::max<int64_t>(4, steps(kMostSortTiles * kSortWaves)) * 64;
+  return {false, (int32_t)std::max<int64_t>(1, ceil_div64(slots, kSortWaves * chunk)), (uint32_t)chunk};
 }
-bool sorts_small(int64_t slots, int32_t groups) { return slots <= kSmallSlots && groups < kSmallBins; }
 
 template <class ID>
 int sort_typed(SortArgs a, hipStream_t st) {
   const int bins = a.groups + 1;
-  if (sorts_small(a.slots, a.groups)) {
-    a.chunk = (uint32_t)ceil_div64(ceil_div64(a.slots, 16), 64) * 64;
-    k_group_small<ID><<<1, 1024, 0, st>>>(a, bits_of(bins));
-    return launched("k_group_small launch");
-  }
-  const SortShape s = sort_shape(a.slots);
+  const SortShape s = sort_shape(a.slots, a.groups);
   a.tiles = s.tiles;
   a.chunk = s.chunk;
-  k_group_count<ID><<<(unsigned)a.tiles, kSortThreads, 0, st>>>(a);
+  if (s.small && s.tiles == 1) {
+    k_group_small<ID, false><<<1, 1024, 0, st>>>(a, bits_of(bins));
+    return launched("k_group_small launch");
+  }
+  if (s.small) {
+    k_group_count<ID, 1024><<<(unsigned)a.tiles, 1024, 0, st>>>(a);
+    if (int rc = launched("k_group_count launch")) return rc;
+    k_group_small<ID, true><<<(unsigned)a.tiles, 1024, 0, st>>>(a, bits_of(bins));
+    return launched("k_group_small launch");
+  }
+  k_group_count<ID, kSortThreads><<<(unsigned)a.tiles, kSortThreads, 0, st>>>(a);
   if (int rc = launched("k_group_count launch")) return rc;
   k_group_tiles<<<(unsigned)ceil_div64(bins, 16), 256, 0, st>>>(a);
   if (int rc = launched("k_group_tiles launch")) return rc;
@@ -556,8 +590,9 @@ int dispatch_pieces(const RowArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t sort_workspace_bytes(int64_t slots, int32_t groups) {
-  if (slots == 0 || sorts_small(slots, groups)) return 0;
-  return (size_t)(sort_shape(slots).tiles + 1) * ((size_t)groups + 1) * sizeof(int32_t);
+  const SortShape s = sort_shape(slots, groups);
+  if (s.small && s.tiles <= 1) return 0;
+  return (size_t)(s.tiles + 1) * ((size_t)groups + 1) * sizeof(int32_t);
 }
 
 int run_sort_groups(int64_t n, int32_t k, int32_t groups, const void* ids, int32_t id_bytes, int64_t ldi,

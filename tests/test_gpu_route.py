@@ -35,14 +35,17 @@ def check_sort(ids, groups):
 @pytest.mark.parametrize("n,k,groups", [
     (1, 1, 1), (1, 8, 64), (63, 1, 3), (64, 1, 2), (65, 1, 70), (48, 4, 64), (1000, 1, 1), (333, 3, 1023),
     (333, 3, 1024), (8192, 1, 20), (8193, 1, 20), (1024, 8, 1023), (2731, 3, 5), (5000, 2, 2047), (5000, 2, 2048),
-    (5000, 2, 2049), (3000, 10, 5000), (20, 2, 65536), (60000, 2, 7), (40000, 8, 128), (5, 3, 0)])
+    (5000, 2, 2049), (3000, 10, 5000), (20, 2, 65536), (60000, 2, 7), (40000, 8, 128), (5, 3, 0), (8193, 1, 1023),
+    (66000, 8, 3), (65536, 8, 3), (65537, 8, 1000)])
 def test_sort(n, k, groups, dtype):
     check_sort(make_ids(n, k, groups, dtype=dtype), groups)
 
 
-def test_sort_many_slots():
-    """More than 1024 a wave: 2.5 million slots, checked with torch's stable sort."""
-    n, k, groups = 250000, 10, 300
+@pytest.mark.parametrize("n,k,groups", [(250000, 10, 300), (262144, 8, 300), (209716, 10, 1000), (300000, 2, 64),
+                                        (200000, 3, 3000)])
+def test_sort_many_slots(n, k, groups):
+    """Up to 2.5 million slots, on both sides of the most that tiles of 8192 hold, checked with
+    torch's stable sort."""
     ids = make_ids(n, k, groups)
     offsets, place = agcn.sort_groups(ids, groups)
     key = torch.where((ids >= 0) & (ids < groups), ids, groups).reshape(-1)
@@ -184,6 +187,11 @@ def test_empty():
     assert torch.equal(offsets, off)
     R = agcn.dispatch(X, place)
     assert R.shape == (0, 8) and agcn.combine(R, place).shape == (0, 8)
+    for groups in (0, 1023, 1024, 5000, 65536):
+        offsets = torch.full((groups + 1,), 7, dtype=torch.int32, device=DEV)
+        ids = torch.zeros((0, 2), dtype=torch.int32, device=DEV)
+        agcn.sort_groups(ids, groups, out=(offsets, ids.clone()))
+        assert not offsets.any()
     offsets, place = agcn.sort_groups(torch.zeros((5, 0), dtype=torch.int32, device=DEV), 3)
     assert torch.equal(offsets, off) and place.shape == (5, 0)
     X = torch.ones((5, 8), device=DEV)
