@@ -14,10 +14,9 @@ int run_int_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, const v
   if (n == 0 || fout == 0) return AGCN_OK;
   const LinearArgs p{n, fin, fout, static_cast<const uint8_t*>(A), lda, nullptr, 0,
                      static_cast<const uint8_t*>(W), ldw, group_w, nullptr, 0, 0, offsets, groups,
-                     Y, ldy, act, SA, SW, group_sw};
+                     Y, ldy, act, SA, SW, group_sw, dtype == AGCN_HALF};
   if (dtype == AGCN_FLOAT) return linear_pieces<kInteger, float>(p, st);
-  if (dtype == AGCN_BFLOAT) return linear_pieces<kInteger, bf16_t>(p, st);
-  return linear_pieces<kInteger, f16_t>(p, st);
+  return linear_pieces<kInteger, uint16_t>(p, st);
 }
 
 }  // namespace agcn

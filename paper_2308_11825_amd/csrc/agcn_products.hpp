@@ -53,7 +53,22 @@ struct LinearArgs {
   int32_t act;
   const float *RA, *RW;  // kInteger: a scale per row of A and of W (group_rw between groups)
   int64_t group_rw;
+  bool half;  // 16-bit results are float16 (TY = uint16_t)
 };
+
+// A result as TY. Integer products write bfloat16 and float16 with the same kernels, as
+// uint16_t, and HALF or `half` says which.
+template <class TY, bool HALF>
+__device__ __forceinline__ TY to_out(float v) {
+  if constexpr (!std::is_same_v<TY, uint16_t>) return (TY)v;
+  else if constexpr (HALF) return __builtin_bit_cast(uint16_t, (f16_t)v);
+  else return __builtin_bit_cast(uint16_t, (bf16_t)v);
+}
+template <class TY>
+__device__ __forceinline__ TY to_out(float v, bool half) {
+  if constexpr (!std::is_same_v<TY, uint16_t>) return (TY)v;
+  else return half ? to_out<TY, true>(v) : to_out<TY, false>(v);
+}
 
 // `valid` of 16 bytes, zeros in the others' place.
 __device__ __forceinline__ v4i load16(const uint8_t* p, int valid) {
@@ -263,7 +278,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_thin(LinearArgs p) {
 #pragma unroll
     for (int k = 1; k < NW; ++k) v += part[k][m][n];
     const Scales<P> more = i < 64 * NW ? scales : Scales<P>(p, rows, n0, m, n);
-    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, more.row, more.column), p.act);
+    if (n0 + n < p.fout) y[m * p.ldy + n] = to_out<TY>(q_act(scales.apply(v, more.row, more.column), p.act), p.half);
   }
 }
 
@@ -398,13 +413,13 @@ struct RowScales {
 
 // Writes RUN neighbouring outputs of a row from column n on, of `count` columns. ALL:
 // the caller knows that they are all there.
-template <bool ALL, int RUN, class TY>
+template <bool ALL, bool HALF, int RUN, class TY>
 __device__ __forceinline__ void store_run(const float (&v)[RUN], TY* to, int n, int count) {
   struct alignas(sizeof(TY)) Run {
     TY e[RUN];
   } o;
 #pragma unroll
-  for (int i = 0; i < RUN; ++i) o.e[i] = (TY)v[i];
+  for (int i = 0; i < RUN; ++i) o.e[i] = to_out<TY, HALF>(v[i]);
   if (ALL || n + RUN <= count) {
     store_any(to + n, o);
   } else {
@@ -414,16 +429,29 @@ __device__ __forceinline__ void store_run(const float (&v)[RUN], TY* to, int n, 
   }
 }
 
-// Calls write(all, relu) with both as compile-time constants: whole tiles without
-// activation, most of them, then write nothing but their values.
-template <class F>
-__device__ __forceinline__ void write_tile(bool whole, int32_t act, F write) {
+// Calls write(all, half, act), constants at compile time where it matters: whole tiles without
+// activation, most of them, then write nothing but their values. half: 16-bit results of
+// TY = uint16_t are float16.
+template <class TY, class F>
+__device__ __forceinline__ void write_tile(const LinearArgs& p, bool whole, F write) {
   using Yes = std::true_type;
   using No = std::false_type;
-  if (whole && act == 0) write(Yes{}, No{});
-  else if (whole) write(Yes{}, Yes{});
-  else if (act == 0) write(No{}, No{});
-  else write(No{}, Yes{});
+  using Relu = std::integral_constant<int32_t, 1>;
+  using None = std::integral_constant<int32_t, 0>;
+  if constexpr (std::is_same_v<TY, uint16_t>) {
+    auto of_type = [&](auto half) {
+      if (whole && p.act == 0) write(Yes{}, half, None{});
+      else if (whole) write(Yes{}, half, Relu{});
+      else write(No{}, half, p.act);
+    };
+    if (p.half) of_type(Yes{});
+    else of_type(No{});
+  } else {
+    if (whole && p.act == 0) write(Yes{}, No{}, None{});
+    else if (whole) write(Yes{}, No{}, Relu{});
+    else if (p.act == 0) write(No{}, No{}, None{});
+    else write(No{}, No{}, Relu{});
+  }
 }
 
 // BM x BN outputs per workgroup of WM x WN waves, TM x TN a wave, one block of 128 k
@@ -527,8 +555,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
   const float* shared = reinterpret_cast<const float*>(lds0);
   static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "scales by threads");
   scales.template share<BM, BN>(reinterpret_cast<float*>(lds0));
-  write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
-    constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
+  write_tile<TY>(p, rows.count == BM && count_n == BN, [&](auto all, auto half, auto act) {
+    constexpr bool ALL = decltype(all)::value, HALF = decltype(half)::value;
     constexpr int kRun = PERM ? 8 : 4;  // neighbouring outputs of a lane
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -541,8 +569,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(LinearArgs p, 
         float v[kRun], column[kRun];
         scales.columns(column, shared + BM + n);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) v[i] = q_act(scales.apply(acc[j + i / 4][t][i % 4], row, column[i]), RELU);
-        store_run<ALL>(v, y + m * p.ldy, n, count_n);
+        for (int i = 0; i < kRun; ++i) v[i] = q_act(scales.apply(acc[j + i / 4][t][i % 4], row, column[i]), act);
+        store_run<ALL, HALF>(v, y + m * p.ldy, n, count_n);
       }
     }
   });
@@ -673,7 +701,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_stream(LinearArgs p) {
 #pragma unroll
     for (int k = 1; k < NW; ++k) v += part[k][m][n];
     const Scales<P> more = i < 64 * NW ? scales : Scales<P>(p, rows, n0, m, n);
-    if (n0 + n < p.fout) y[m * p.ldy + n] = (TY)q_act(scales.apply(v, more.row, more.column), p.act);
+    if (n0 + n < p.fout) y[m * p.ldy + n] = to_out<TY>(q_act(scales.apply(v, more.row, more.column), p.act), p.half);
   }
 }
 
@@ -909,8 +937,8 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
   TY* y = static_cast<TY*>(p.Y) + rows.row * p.ldy + n0;
   const float* shared = reinterpret_cast<const float*>(lds + 4 * 32 * kRow);
   scales.template share<BM, BN>(reinterpret_cast<float*>(lds + 4 * 32 * kRow));
-  write_tile(rows.count == BM && count_n == BN, p.act, [&](auto all, auto relu) {
-    constexpr bool ALL = decltype(all)::value, RELU = decltype(relu)::value;
+  write_tile<TY>(p, rows.count == BM && count_n == BN, [&](auto all, auto half, auto act) {
+    constexpr bool ALL = decltype(all)::value, HALF = decltype(half)::value;
     struct alignas(16) Run {
       TY e[kRun];
     };
@@ -927,7 +955,7 @@ __global__ __launch_bounds__(256, H == 64 ? 1 : 2) void k_qlinear_ring(LinearArg
           float column[kRun];
           scales.columns(column, shared + BM + wn * 2 * H + n);
 #pragma unroll
-          for (int i = 0; i < kRun; ++i) v.e[i] = (TY)q_act(scales.apply(acc[j][t][c + i], scale, column[i]), RELU);
+          for (int i = 0; i < kRun; ++i) v.e[i] = to_out<TY, HALF>(q_act(scales.apply(acc[j][t][c + i], scale, column[i]), act));
           *reinterpret_cast<Run*>(own + r * kRow + n * sizeof(TY)) = v;
         }
       const int n = lane % kLanes * kRun, left = count_n - wn * 2 * H - n, row0 = wm * 2 * H + t * 32 + lane / kLanes;

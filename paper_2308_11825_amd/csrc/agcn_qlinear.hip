@@ -27,7 +27,7 @@ int run_quantized_linear(int64_t n, int32_t fin, int32_t fout, int32_t groups, c
   const LinearArgs p{n, fin, fout, static_cast<const uint8_t*>(A), lda,
                      static_cast<const uint8_t*>(SA), ldsa, static_cast<const uint8_t*>(W), ldw,
                      group_w, static_cast<const uint8_t*>(SW), ldsw, group_sw, offsets, groups, Y,
-                     ldy, act, nullptr, nullptr, 0};
+                     ldy, act, nullptr, nullptr, 0, false};
   if (dtype == AGCN_FLOAT) return linear_pieces<kExact, float>(p, st);
   if (dtype == AGCN_BFLOAT) return linear_pieces<kFast, bf16_t>(p, st);
   return linear_pieces<kExact, f16_t>(p, st);

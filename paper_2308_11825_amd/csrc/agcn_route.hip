@@ -280,6 +280,7 @@ struct RowArgs {
   int64_t ldo;
   float* dw;
   int64_t lddw;
+  bool past;  // the slots' rows and the results start on lines
 };
 
 // The row that a place names, and whether its slot is kept; places outside the matrix name
@@ -308,7 +309,7 @@ __device__ __forceinline__ int64_t token_of(int64_t i) {
 // a row ends where the row does).
 template <int W>
 using Bytes = std::conditional_t<W == 16, v4i_any, std::conditional_t<W == 4, uint32_t, uint8_t>>;
-template <int W, int G, int U, bool PAST>
+template <int W, int G, int U>
 __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
   const int lane = threadIdx.x % G;
   for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (u > 0 && at + u * G * W >= a.f) break;
-          store_row<PAST>(to + from[u], s.kept ? v[u] : Bytes<W>{});
+          store_row(to + from[u], s.kept ? v[u] : Bytes<W>{}, a.past);
         }
       }
     }
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
 
 // out[t] = sum over c of w[t][c] R[place[t][c]], in c's order, A rows and U pieces of each on
 // their way at a time.
-template <class T, int V, int G, int U, int A, bool PAST>
+template <class T, int V, int G, int U, int A>
 __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
   using P = Piece<T, V>;
   const int lane = threadIdx.x % G;
@@ -365,9 +366,7 @@ __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
           const Slot s(a, t, c);
           kept[u] = s.kept && c0 + u < a.k;
           w[u] = a.w != nullptr ? a.w[t * a.ldw + c] : 1.0f;
-          const T* r = static_cast<const T*>(a.R) + s.row * a.ldr;
-#pragma unroll
-          for (int x = 0; x < U; ++x) v[u][x] = load_row<P, PAST>(r + from[x]);
+          load_row(v[u], static_cast<const T*>(a.R) + s.row * a.ldr, from, a.past);
         }
 #pragma unroll
         for (int u = 0; u < A; ++u)
@@ -383,7 +382,7 @@ __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
         P o;
 #pragma unroll
         for (int e = 0; e < V; ++e) o.e[e] = (T)sum[x][e];
-        store_row<PAST>(static_cast<T*>(a.out) + t * a.ldo + from[x], o);
+        store_row(static_cast<T*>(a.out) + t * a.ldo + from[x], o, a.past);
       }
     }
   }
@@ -391,7 +390,7 @@ __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
 
 // dR[place[t][c]] = w[t][c] X[t] and dw[t][c] = X[t] . R[place[t][c]], X the gradient of
 // k_combine's sum. A group of lanes has a whole token, A slots and U pieces of each at a time.
-template <class T, int V, int G, int U, int A, bool PAST>
+template <class T, int V, int G, int U, int A>
 __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
   using P = Piece<T, V>;
   const int lane = threadIdx.x % G;
@@ -421,10 +420,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
           x[y] = load_any<P>(static_cast<const T*>(a.X) + t * a.ldx + from[y]);
         }
 #pragma unroll
-        for (int u = 0; u < A; ++u)
-#pragma unroll
-          for (int y = 0; y < U; ++y)
-            r[u][y] = load_row<P, PAST>(static_cast<const T*>(a.R) + row[u] * a.ldr + from[y]);
+        for (int u = 0; u < A; ++u) load_row(r[u], static_cast<const T*>(a.R) + row[u] * a.ldr, from, a.past);
 #pragma unroll
         for (int y = 0; y < U; ++y) {
           if (y > 0 && at + y * G * V >= a.f) break;
@@ -438,7 +434,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
               o.e[e] = (T)(kept[u] ? w[u] * g : 0.0f);
               dot[u] = e >= shared ? fmaf(g, to_float(r[u][y].e[e]), dot[u]) : dot[u];
             }
-            if (inside[u]) store_row<PAST>(static_cast<T*>(a.out) + row[u] * a.ldo + from[y], o);
+            if (inside[u]) store_row(static_cast<T*>(a.out) + row[u] * a.ldo + from[y], o, a.past);
           }
         }
       }
@@ -533,57 +529,56 @@ void slots_at_once(int32_t k, F use) {
   else use(std::integral_constant<int, 4>{});
 }
 
-template <class T, int V, bool PAST>
+template <class T, int V>
 int combine_pieces(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = ceil_div64(a.f, V);
   slots_at_once(a.k, [&](auto at_once) {
     constexpr int A = decltype(at_once)::value;
     // Rows over 4 KB: the lanes of four waves, two pieces each.
     if (V > 1 && pieces > 256) {
-      k_combine<T, V, 256, 2, A, PAST><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+      k_combine<T, V, 256, 2, A><<<row_grid<256>(a.n), 256, 0, st>>>(a);
       return;
     }
     token_shape<V == 1>(pieces, [&](auto shape) {
       constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
-      k_combine<T, V, G, U, A, PAST><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+      k_combine<T, V, G, U, A><<<row_grid<G>(a.n), 256, 0, st>>>(a);
     });
   });
   return launched("k_combine launch");
 }
-template <class T, int V, bool PAST>
+template <class T, int V>
 int combine_grad_pieces(const RowArgs& a, hipStream_t st) {
   slots_at_once(a.k, [&](auto at_once) {
     constexpr int A = decltype(at_once)::value;
     token_shape<V == 1>(ceil_div64(a.f, V), [&](auto shape) {
       constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
-      k_combine_grad<T, V, G, U, A, PAST><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+      k_combine_grad<T, V, G, U, A><<<row_grid<G>(a.n), 256, 0, st>>>(a);
     });
   });
   return launched("k_combine_grad launch");
 }
 
 template <class T>
-int combine_typed(const RowArgs& a, bool grad, hipStream_t st) {
+int combine_typed(RowArgs a, bool grad, hipStream_t st) {
   constexpr int V = kPiece<T>;
-  if (a.f < V) return grad ? combine_grad_pieces<T, 1, false>(a, st) : combine_pieces<T, 1, false>(a, st);
-  const bool past = on_lines(a.R, a.ldr, sizeof(T)) && on_lines(a.out, a.ldo, sizeof(T));
-  if (grad) return past ? combine_grad_pieces<T, V, true>(a, st) : combine_grad_pieces<T, V, false>(a, st);
-  return past ? combine_pieces<T, V, true>(a, st) : combine_pieces<T, V, false>(a, st);
+  a.past = on_lines(a.R, a.ldr, sizeof(T)) && on_lines(a.out, a.ldo, sizeof(T));
+  if (a.f < V) return grad ? combine_grad_pieces<T, 1>(a, st) : combine_pieces<T, 1>(a, st);
+  return grad ? combine_grad_pieces<T, V>(a, st) : combine_pieces<T, V>(a, st);
 }
 int combine_any(const RowArgs& a, int32_t dtype, bool grad, hipStream_t st) {
   if (dtype == AGCN_FLOAT) return combine_typed<float>(a, grad, st);
   return dtype == AGCN_BFLOAT ? combine_typed<bf16_t>(a, grad, st) : combine_typed<f16_t>(a, grad, st);
 }
 
-template <int W, bool PAST>
+template <int W>
 int dispatch_pieces(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = ceil_div64(a.f, W);
-  if (pieces <= 1) k_dispatch<W, 1, 1, PAST><<<row_grid<1>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 4) k_dispatch<W, 4, 1, PAST><<<row_grid<4>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 16 || W < 16) k_dispatch<W, 16, 1, PAST><<<row_grid<16>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 64) k_dispatch<W, 64, 1, PAST><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 128) k_dispatch<W, 64, 2, PAST><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else k_dispatch<W, 256, 2, PAST><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  if (pieces <= 1) k_dispatch<W, 1, 1><<<row_grid<1>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 4) k_dispatch<W, 4, 1><<<row_grid<4>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 16 || W < 16) k_dispatch<W, 16, 1><<<row_grid<16>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 64) k_dispatch<W, 64, 1><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else if (pieces <= 128) k_dispatch<W, 64, 2><<<row_grid<64>(a.n), 256, 0, st>>>(a);
+  else k_dispatch<W, 256, 2><<<row_grid<256>(a.n), 256, 0, st>>>(a);
   return launched("k_dispatch launch");
 }
 
@@ -607,8 +602,9 @@ int run_dispatch(int64_t n, int32_t k, int64_t bytes, const void* X, int64_t ldx
   if (n == 0 || k == 0 || bytes == 0) return AGCN_OK;
   RowArgs a{};
   a.n = n, a.f = bytes, a.k = k, a.place = place, a.ldp = ldp, a.X = X, a.ldx = ldx, a.out = Y, a.ldo = ldy;
-  if (bytes >= 16) return on_lines(Y, ldy, 1) ? dispatch_pieces<16, true>(a, st) : dispatch_pieces<16, false>(a, st);
-  return bytes >= 4 ? dispatch_pieces<4, false>(a, st) : dispatch_pieces<1, false>(a, st);
+  a.past = on_lines(Y, ldy, 1);
+  if (bytes >= 16) return dispatch_pieces<16>(a, st);
+  return bytes >= 4 ? dispatch_pieces<4>(a, st) : dispatch_pieces<1>(a, st);
 }
 
 int run_combine(int64_t n, int32_t k, int32_t f, int32_t dtype, const void* R, int64_t ldr, const int32_t* place,

@@ -39,6 +39,30 @@ __device__ __forceinline__ void store_row(T* p, const V& v) {
     store_any(p, v);
   }
 }
+// The same decided when it runs, for kernels of many shapes. (Between the two empty statements
+// nothing is moved: the compiler would make one access of both ways, and an ordinary one.)
+template <int N, class V, class T, class At>
+__device__ __forceinline__ void load_row(V (&v)[N], const T* p, const At (&at)[N], bool past) {
+  if (past) {
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = load_row<V, true>(p + at[i]);
+    asm volatile("");
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = load_any<V>(p + at[i]);
+  }
+}
+template <class T, class V>
+__device__ __forceinline__ void store_row(T* p, const V& v, bool past) {
+  if (past) {
+    asm volatile("");
+    store_row<true>(p, v);
+    asm volatile("");
+  } else {
+    store_any(p, v);
+  }
+}
 // Rows of `size` bytes a value that start on lines; no row there, or one of them only, are in line.
 inline bool on_lines(const void* p, int64_t ld, int64_t size) {
   return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 128 == 0 && ld * size % 128 == 0);
