@@ -3,6 +3,11 @@
 // with one W, or with a W for each group of rows (agcn_grouped_int_linear). The sum is
 // exact in 32 bits for fewer than 2^17 values of k (each product is 2^14 at most), and is
 // rounded once to fp32 and once by each scale.
+//
+// The kernels are those of agcn_products.hpp with the matrix cores' integer instructions, as many
+// cycles as the e4m3 ones. Where the matrix cores bound them, power does: 16384 x 8192 -> 8192 874 to 975 us, 2.3
+// to 2.5 POP/s, with the matrix cores at work in 66 % of the cycles of a clock that falls to 1.6 GHz;
+// 32768 x 4096 -> 2048 258 us, and 241 for zeros. 1 x 4096 -> 4096 4.7 us.
 #include "agcn_products.hpp"
 
 namespace agcn {

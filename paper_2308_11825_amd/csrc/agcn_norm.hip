@@ -6,7 +6,11 @@
 //   dx = rs (d - sum d / f - xh sum(d xh) / f) + dh,  dg = sum over rows of dy xh,
 //   db = sum over rows of dy.
 //
-// Little to do but read and write: a row is read once and held in registers.
+// Little to do but read and write: a row is read once and held in registers, and memory bounds
+// the time of more rows than a chip holds. us on one MI355X: 32768 x 8192 bfloat16 with residual 377
+// (5.7 TB/s), 230,000 x 128 float32 76 (6.2); gradients with the residual stream's 362 and 77 (5.9, 6.1),
+// 60,000 x 601 float16 without 49 (4.4: its rows share lines); 40,000 columns, past registers, 2.3 to 3. A copy of 2^30 bytes reaches 5.1, one
+// that goes past the caches with a workgroup for every 4 KB 6.4.
 #include <algorithm>
 #include <cfloat>
 
@@ -27,6 +31,7 @@ struct NormArgs {
   int64_t ldh;
   const void* g;
   const void* b;  // or NULL
+  bool p_float;   // g and b are float32, else of the rows' type
   float eps;
   void* Y;
   int64_t ldy;
@@ -126,6 +131,24 @@ __device__ __forceinline__ void write_stats(float* to, const RowStats& s, float 
   to[1] = s.rs == 0.0f ? 1.0f / sqrtf(eps) : s.rs * s.scale;
 }
 
+// Parameters of V columns from `at` on.
+template <class T, int V>
+__device__ __forceinline__ void load_params(float (&to)[V], const void* p, int at, bool p_float) {
+  if (p_float) {
+    const auto v = load_any<Piece<float, V>>(static_cast<const float*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = v.e[i];
+  } else {
+    const auto v = load_any<Piece<T, V>>(static_cast<const T*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = to_float(v.e[i]);
+  }
+}
+template <class T>
+__device__ __forceinline__ float load_param(const void* p, int64_t at, bool p_float) {
+  return p_float ? static_cast<const float*>(p)[at] : to_float(static_cast<const T*>(p)[at]);
+}
+
 // One row per G lanes, NV pieces of V columns a lane (V <= f <= G * NV * V, or V = 1); the
 // parameters of its columns stay in registers too.
 template <class T, class TP, int G, int NV, int V, bool PAST>
@@ -184,7 +207,10 @@ __global__ __launch_bounds__(row_threads(G)) void k_layer_norm(NormArgs a) {
     T* y = static_cast<T*>(a.Y) + row * a.ldy;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (!kKeep) params(v);
+      if constexpr (!kKeep) {
+        if (NV * V >= 32) asm volatile("" ::: "memory");  // (not all pieces' at once: no registers for them)
+        params(v);
+      }
       if (shared[v] == V) continue;
       // (H after the statistics: where it lies on X or R, all lanes have read their columns.)
       if (a.H != nullptr) {
@@ -202,9 +228,10 @@ __global__ __launch_bounds__(row_threads(G)) void k_layer_norm(NormArgs a) {
 }
 
 // Rows too long for registers: one workgroup a row, its values read three times.
-template <class T, class TP>
+template <class T>
 __global__ __launch_bounds__(1024) void k_layer_norm_long(NormArgs a) {
-  constexpr int G = 1024, V = 8;
+  constexpr int G = 1024, V = kPiece<T>;
+  using In = Piece<T, V>;
   __shared__ float part[2][16];
   auto block_sum = [&](float v, int at) {
     v = lanes_sum<64>(v);
@@ -219,10 +246,15 @@ __global__ __launch_bounds__(1024) void k_layer_norm_long(NormArgs a) {
       for (int64_t c = threadIdx.x * V; c < a.f; c += G * V) {
         const int valid = (int)std::min<int64_t>(V, a.f - c);
         float h[V];
+        if (valid == V) {
+          const In v = load_any<In>(x + c);
+          In add = {};
+          if (a.R != nullptr) add = load_any<In>(r + c);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          h[i] = i < valid ? to_float(x[c + i]) : 0.0f;
-          if (a.R != nullptr && i < valid) h[i] += to_float(r[c + i]);
+          for (int i = 0; i < V; ++i) h[i] = to_float(v.e[i]) + (a.R != nullptr ? to_float(add.e[i]) : 0.0f);
+        } else {
+          for (int i = 0; i < V; ++i)
+            h[i] = i < valid ? to_float(x[c + i]) + (a.R != nullptr ? to_float(r[c + i]) : 0.0f) : 0.0f;
         }
         use(c, valid, h);
       }
@@ -259,13 +291,26 @@ __global__ __launch_bounds__(1024) void k_layer_norm_long(NormArgs a) {
     if (!stats(1.0f, &s)) stats(kTiny, &s);
     if (a.stats != nullptr && threadIdx.x == 0) write_stats(a.stats + row * a.lds, s, a.eps);
     each([&](int64_t c, int valid, const float(&h)[V]) {
+      T* to = static_cast<T*>(a.Y) + row * a.ldy + c;
+      T* hidden = static_cast<T*>(a.H) + row * a.ldh + c;
+      if (valid == V) {
+        float g[V], b[V] = {};
+        load_params<T>(g, a.g, (int)c, a.p_float);
+        if (a.b != nullptr) load_params<T>(b, a.b, (int)c, a.p_float);
+        In y, o;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (i >= valid) break;
-        if (a.H != nullptr) static_cast<T*>(a.H)[row * a.ldh + c + i] = (T)h[i];
-        const float b = a.b != nullptr ? to_float(static_cast<const TP*>(a.b)[c + i]) : 0.0f;
-        static_cast<T*>(a.Y)[row * a.ldy + c + i] =
-            (T)fmaf(s(h[i]), to_float(static_cast<const TP*>(a.g)[c + i]), b);
+        for (int i = 0; i < V; ++i) {
+          o.e[i] = (T)h[i];
+          y.e[i] = (T)fmaf(s(h[i]), g[i], b[i]);
+        }
+        if (a.H != nullptr) store_any(hidden, o);
+        store_any(to, y);
+      } else {
+        for (int i = 0; i < valid; ++i) {
+          if (a.H != nullptr) hidden[i] = (T)h[i];
+          const float b = a.b != nullptr ? load_param<T>(a.b, c + i, a.p_float) : 0.0f;
+          to[i] = (T)fmaf(s(h[i]), load_param<T>(a.g, c + i, a.p_float), b);
+        }
       }
     });
   }
@@ -285,6 +330,7 @@ struct GradArgs {
   const float* stats;
   int64_t lds;
   const void* g;
+  bool p_float;  // g is float32, else of the rows' type
   void* dX;
   int64_t lddx;
   float* part;  // [workgroups][2][f]: the workgroup's sums of dy xh and of dy
@@ -299,12 +345,12 @@ struct Normalised {
 };
 
 // Rows as in k_layer_norm, each workgroup over every gridDim.x-th; the columns' sums stay in
-// registers until the end.
-template <class T, class TP, int G, int NV, int V, bool PAST>
+// registers until the end, and k_layer_norm_sums adds the workgroups' up: 4 to 6 us more, a
+// third of the time of 2048 x 4096 (25 us).
+template <class T, int G, int NV, int V, bool PAST>
 __global__ __launch_bounds__(row_threads(G)) void k_layer_norm_grad(GradArgs a) {
   constexpr int kThreads = row_threads(G), kRows = kThreads / G, kWaves = G > 64 ? G / 64 : 1;
   using In = Piece<T, V>;
-  using Param = Piece<TP, V>;
   __shared__ float part[2][16][2];
   const int lane = threadIdx.x % G;
   int start[NV], shared[NV];
@@ -314,12 +360,9 @@ __global__ __launch_bounds__(row_threads(G)) void k_layer_norm_grad(GradArgs a) 
     const Column<G, V> c(v, lane, a.f);
     start[v] = c.start;
     shared[v] = c.shared;
-    const Param p = load_any<Param>(static_cast<const TP*>(a.g) + c.start);
+    load_params<T>(g[v], a.g, c.start, a.p_float);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      g[v][i] = to_float(p.e[i]);
-      dg[v][i] = db[v][i] = 0.0f;
-    }
+    for (int i = 0; i < V; ++i) dg[v][i] = db[v][i] = 0.0f;
   }
   const float over = 1.0f / (float)a.f;
   int turn = 0;
@@ -429,17 +472,16 @@ __global__ __launch_bounds__(row_threads(G)) void k_layer_norm_grad(GradArgs a) 
 }
 
 // Rows too long for registers: dx, one workgroup a row.
-template <class T, class TP>
+template <class T>
 __global__ __launch_bounds__(1024) void k_layer_norm_grad_long(GradArgs a) {
   __shared__ float part[2][16];
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const T* dy = static_cast<const T*>(a.dY) + row * a.lddy;
     const T* h = static_cast<const T*>(a.H) + row * a.ldh;
-    const TP* g = static_cast<const TP*>(a.g);
     const Normalised norm(a.stats + row * a.lds);
     float s1 = 0.0f, s2 = 0.0f;
     for (int c = threadIdx.x; c < a.f; c += 1024) {
-      const float d = to_float(dy[c]) * to_float(g[c]);
+      const float d = to_float(dy[c]) * load_param<T>(a.g, c, a.p_float);
       s1 += d;
       s2 = fmaf(d, norm(to_float(h[c])), s2);
     }
@@ -455,7 +497,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_grad_long(GradArgs a) {
     s1 = sum16(part[0][threadIdx.x % 16]) * over;
     s2 = sum16(part[1][threadIdx.x % 16]) * over;
     for (int c = threadIdx.x; c < a.f; c += 1024) {
-      float d = norm.rs * (fmaf(to_float(dy[c]), to_float(g[c]), -s1) - norm(to_float(h[c])) * s2);
+      float d = norm.rs * (fmaf(to_float(dy[c]), load_param<T>(a.g, c, a.p_float), -s1) - norm(to_float(h[c])) * s2);
       if (a.dH != nullptr) d += to_float(static_cast<const T*>(a.dH)[row * a.lddh + c]);
       static_cast<T*>(a.dX)[row * a.lddx + c] = (T)d;
     }
@@ -503,23 +545,31 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(int32_t parts, int32_t
   }
 }
 
-// Workgroups of a launch, at most; rows past them are looped over. Where rows start on lines, one
-// for every few rows (50,000 x 2048 bfloat16 134 us, and 150 with 2048 workgroups), unless
-// the parameters (over 2^15 bytes) are better kept in registers over several rows than read
-// again (32768 x 8192 bfloat16 381 us, and 439). Other rows share lines, which L2 puts together as long as
-// they are written close by: 60,000 x 601 float16 66 us, 72 with a workgroup for every row.
-constexpr int64_t kNormGroups = 1024, kSharedGroups = 8192, kMostNormGroups = 1 << 20, kLongRowGroups = 1024;
+// Workgroups of a launch, at most; rows past them are looped over, with the parameters kept in
+// registers. That pays where the parameters are more than half of what a row moves (50,000 x 2048
+// bfloat16 without residual 75 us with 2048 workgroups and 103 with one a row; 60,000 x 640 of one wave a
+// row 37 with 4096 and 46), where rows share lines, which L2 puts together as long as they are written
+// close by (60,000 x 601 float16 69 and 76), and for wide rows of 16 bits with their long chains of
+// loads (16384 x 8192 bfloat16 184 with 1024 and 202; 57,522 x 2432 203 with 2048 and 243). Other rows do better with a
+// workgroup for every few (50,000 x 1024 float32 130 us, and 145 with 2048; 20,000 x 5120 269 and 299).
+constexpr int64_t kMostNormGroups = 1 << 20, kLongRowGroups = 1024;
+template <class T, int G, int NV>
+int64_t most_groups(const NormArgs& a, bool past) {
+  if (G * NV > 256 && sizeof(T) < 4) return G <= 256 ? 2048 : 1024;
+  const int64_t row = (int64_t)(a.R != nullptr ? 4 : 2) * a.f * (int64_t)sizeof(T);
+  const int64_t params = (int64_t)(a.b != nullptr ? 2 : 1) * a.f * (int64_t)(a.p_float ? sizeof(float) : sizeof(T));
+  if (past && row >= 2 * params) return kMostNormGroups;
+  return G <= 64 ? 4096 : G <= 256 ? 2048 : 1024;
+}
 
 template <class T, class TP, int V, bool PAST>
 int norm_pieces(const NormArgs& a, hipStream_t st) {
-  const bool wide = 2 * (int64_t)a.f * (int64_t)sizeof(TP) > 32768;
-  const int64_t most = !PAST ? kSharedGroups : wide ? kNormGroups : kMostNormGroups;
-  const bool fits = row_shape<V == 1, false>(ceil_div64(a.f, V), [&](auto shape) {
+  const bool fits = row_shape<V, false>(ceil_div64(a.f, V), [&](auto shape) {
     constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV, kThreads = row_threads(G);
-    const int64_t grid = std::min<int64_t>(most, ceil_div64(a.n, kThreads / G));
+    const int64_t grid = std::min(most_groups<T, G, NV>(a, PAST), ceil_div64(a.n, kThreads / G));
     k_layer_norm<T, TP, G, NV, V, PAST><<<(unsigned)grid, kThreads, 0, st>>>(a);
   });
-  if (!fits) k_layer_norm_long<T, TP><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
+  if (!fits) k_layer_norm_long<T><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
   return launched("k_layer_norm launch");
 }
 
@@ -536,41 +586,51 @@ int norm_typed(const NormArgs& a, hipStream_t st) {
 // 256; 8192 x 16384 float16 190 with 256 and 223 with 512).
 int64_t grad_groups(int64_t n, int32_t f, int64_t v) {
   int64_t groups = 0;
-  if (row_shape<false, true>(ceil_div64(f, v), [&](auto shape) {
-        constexpr int G = decltype(shape)::kG, kRows = row_threads(G) / G;
-        groups = std::min<int64_t>(G == 1024 ? 256 : 512, ceil_div64(n, 2 * kRows));
-      }))
+  auto set = [&](auto shape) {
+    constexpr int G = decltype(shape)::kG, kRows = row_threads(G) / G;
+    groups = std::min<int64_t>(G == 1024 ? 256 : 512, ceil_div64(n, 2 * kRows));
+  };
+  const int64_t pieces = ceil_div64(f, v);
+  if (v == 1 ? row_shape<1, true>(pieces, set) : v == 4 ? row_shape<4, true>(pieces, set) : row_shape<8, true>(pieces, set))
     return groups;
   return std::min<int64_t>(n, std::max<int64_t>(1, 2048 / ceil_div64(f, 256)));
 }
 
-template <class T, class TP, int V, bool PAST>
-int grad_pieces(const GradArgs& a, TP* dg, TP* db, hipStream_t st) {
+template <class T>
+int column_sums(const GradArgs& a, int64_t groups, void* dg, void* db, hipStream_t st) {
+  const unsigned grid = (unsigned)ceil_div64(2 * (int64_t)a.f, 32);
+  if (a.p_float)
+    k_layer_norm_sums<<<grid, 1024, 0, st>>>((int32_t)groups, a.f, a.part, static_cast<float*>(dg),
+                                             static_cast<float*>(db));
+  else
+    k_layer_norm_sums<<<grid, 1024, 0, st>>>((int32_t)groups, a.f, a.part, static_cast<T*>(dg), static_cast<T*>(db));
+  return launched("k_layer_norm_sums launch");
+}
+
+template <class T, int V, bool PAST>
+int grad_pieces(const GradArgs& a, void* dg, void* db, hipStream_t st) {
   const int64_t groups = grad_groups(a.n, a.f, V);
-  const bool fits = row_shape<V == 1, true>(ceil_div64(a.f, V), [&](auto shape) {
+  const bool fits = row_shape<V, true>(ceil_div64(a.f, V), [&](auto shape) {
     constexpr int G = decltype(shape)::kG, NV = decltype(shape)::kNV;
-    k_layer_norm_grad<T, TP, G, NV, V, PAST><<<(unsigned)groups, row_threads(G), 0, st>>>(a);
+    k_layer_norm_grad<T, G, NV, V, PAST><<<(unsigned)groups, row_threads(G), 0, st>>>(a);
   });
   if (!fits) {
-    k_layer_norm_grad_long<T, TP><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
+    k_layer_norm_grad_long<T><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
     if (int rc = launched("k_layer_norm_grad_long launch")) return rc;
     if (a.part != nullptr)
       k_layer_norm_columns<T><<<dim3((unsigned)ceil_div64(a.f, 256), (unsigned)groups), 256, 0, st>>>(a);
   }
   if (int rc = launched("k_layer_norm_grad launch")) return rc;
   if (a.part == nullptr) return AGCN_OK;
-  k_layer_norm_sums<TP><<<(unsigned)ceil_div64(2 * (int64_t)a.f, 32), 1024, 0, st>>>((int32_t)groups, a.f, a.part,
-                                                                                    dg, db);
-  return launched("k_layer_norm_sums launch");
+  return column_sums<T>(a, groups, dg, db, st);
 }
 
-template <class T, class TP>
+template <class T>
 int grad_typed(const GradArgs& a, void* dg, void* db, hipStream_t st) {
-  TP *g = static_cast<TP*>(dg), *b = static_cast<TP*>(db);
-  if (a.f < kPiece<T>) return grad_pieces<T, TP, 1, false>(a, g, b, st);
+  if (a.f < kPiece<T>) return grad_pieces<T, 1, false>(a, dg, db, st);
   const bool past = on_lines(a.dY, a.lddy, sizeof(T)) && on_lines(a.H, a.ldh, sizeof(T)) &&
                     on_lines(a.dH, a.lddh, sizeof(T)) && on_lines(a.dX, a.lddx, sizeof(T));
-  return past ? grad_pieces<T, TP, kPiece<T>, true>(a, g, b, st) : grad_pieces<T, TP, kPiece<T>, false>(a, g, b, st);
+  return past ? grad_pieces<T, kPiece<T>, true>(a, dg, db, st) : grad_pieces<T, kPiece<T>, false>(a, dg, db, st);
 }
 
 template <class TP>
@@ -599,11 +659,10 @@ int run_layer_norm(int64_t n, int32_t f, int32_t dtype, const void* X, int64_t l
                    void* H, int64_t ldh, const void* g, const void* b, int32_t p_dtype, float eps, void* Y,
                    int64_t ldy, float* stats, int64_t lds, hipStream_t st) {
   if (n == 0 || f == 0) return AGCN_OK;
-  const NormArgs a{n, f, X, ldx, R, ldr, H, ldh, g, b, eps, Y, ldy, stats, lds};
+  const NormArgs a{n, f, X, ldx, R, ldr, H, ldh, g, b, p_dtype == AGCN_FLOAT, eps, Y, ldy, stats, lds};
   if (dtype == AGCN_FLOAT) return norm_typed<float, float>(a, st);
-  if (dtype == AGCN_BFLOAT)
-    return p_dtype == AGCN_FLOAT ? norm_typed<bf16_t, float>(a, st) : norm_typed<bf16_t, bf16_t>(a, st);
-  return p_dtype == AGCN_FLOAT ? norm_typed<f16_t, float>(a, st) : norm_typed<f16_t, f16_t>(a, st);
+  if (dtype == AGCN_BFLOAT) return a.p_float ? norm_typed<bf16_t, float>(a, st) : norm_typed<bf16_t, bf16_t>(a, st);
+  return a.p_float ? norm_typed<f16_t, float>(a, st) : norm_typed<f16_t, f16_t>(a, st);
 }
 
 int run_layer_norm_backward(int64_t n, int32_t f, int32_t dtype, const void* dY, int64_t lddy, const void* H,
@@ -617,12 +676,10 @@ int run_layer_norm_backward(int64_t n, int32_t f, int32_t dtype, const void* dY,
     if (p_dtype == AGCN_FLOAT) return zeros<float>(f, dg, db, st);
     return p_dtype == AGCN_BFLOAT ? zeros<bf16_t>(f, dg, db, st) : zeros<f16_t>(f, dg, db, st);
   }
-  const GradArgs a{n, f, dY, lddy, H, ldh, dH, lddh, stats, lds, g, dX, lddx,
+  const GradArgs a{n, f, dY, lddy, H, ldh, dH, lddh, stats, lds, g, p_dtype == AGCN_FLOAT, dX, lddx,
                    sums ? static_cast<float*>(ws) : nullptr};
-  if (dtype == AGCN_FLOAT) return grad_typed<float, float>(a, dg, db, st);
-  if (dtype == AGCN_BFLOAT)
-    return p_dtype == AGCN_FLOAT ? grad_typed<bf16_t, float>(a, dg, db, st) : grad_typed<bf16_t, bf16_t>(a, dg, db, st);
-  return p_dtype == AGCN_FLOAT ? grad_typed<f16_t, float>(a, dg, db, st) : grad_typed<f16_t, f16_t>(a, dg, db, st);
+  if (dtype == AGCN_FLOAT) return grad_typed<float>(a, dg, db, st);
+  return dtype == AGCN_BFLOAT ? grad_typed<bf16_t>(a, dg, db, st) : grad_typed<f16_t>(a, dg, db, st);
 }
 
 }  // namespace agcn

@@ -158,7 +158,7 @@ __device__ __forceinline__ void block_products(Sum4<P> (&acc)[NT][MT], GetW w, G
 // its column's. Sums that nothing was added to are 0 whatever the scales. A thread asks for
 // the scales of one row and one column of the tile before the products and passes them on
 // through LDS after them: asked for where they are needed, they cost a 256 x 256 tile 32 loads one
-// after the other (32768 x 4096 -> 2048 SCALES_BEFORE us, SCALES_NOW now).
+// after the other (32768 x 4096 -> 2048 288 us, and 258 this way).
 template <Products P>
 struct Scales {
   float row = 0.0f, column = 0.0f;
@@ -1053,7 +1053,7 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
       return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     }
     // Few outputs and no rows to stage: the k of an output over eight waves. 5000 x 602 -> 41 over
-    // 7 groups THIN_NOW us, 12.5 in 64 x 64 tiles. (Integer sums are the same in any order.)
+    // 7 groups 7.9 us, 12.5 in 64 x 64 tiles. (Integer sums are the same in any order.)
     if (P == kInteger && fits_y && few_rows_grid(p.n, p.groups, 32, GROUPED) * ceil_div64(p.fout, 16) <= 4 * kUnits)
       return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     if (!near) return fail(AGCN_ERR_UNSUPPORTED, "row strides over 8 million bytes and over 65535 row tiles");

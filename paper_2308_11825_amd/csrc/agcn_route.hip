@@ -84,6 +84,9 @@ __device__ __forceinline__ int block_scan(int v, int* part, int* total) {
   return before + in - v;
 }
 
+// Sorting takes its launches' time and little more: 192 slots 3.6 us, 262,144 11.6 in two launches
+// (16.6 in three), 10^6 18.
+//
 // Up to kSmallSlots slots: one workgroup, each wave a run of the slots. A slot's rank among its
 // wave's slots of its group, then the waves' and the groups' sums. TILED: a workgroup for each
 // tile of up to that many slots, the groups' counts in all tiles having been written before;
@@ -306,7 +309,11 @@ __device__ __forceinline__ int64_t token_of(int64_t i) {
 }
 
 // A row read once and written k times, U pieces of W bytes a lane at a time (the last piece of
-// a row ends where the row does).
+// a row ends where the row does). Reading a row for each place costs more: the writes are in order,
+// but the same row is fetched k times (32768 rows of 8 KB to 8 places each 570 us, 416 this way, 5.8
+// TB/s; 478 with ordinary stores). Rows that share lines: neighbours in group order come from neighbouring
+// rows, which go to one XCD, and their parts of a line meet in its L2 (100,000 x 6 x 600 bytes 93 us, 127
+// with workgroups as they come).
 template <int W>
 using Bytes = std::conditional_t<W == 16, v4i_any, std::conditional_t<W == 4, uint32_t, uint8_t>>;
 template <int W, int G, int U>
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
 }
 
 // out[t] = sum over c of w[t][c] R[place[t][c]], in c's order, A rows and U pieces of each on
-// their way at a time.
+// their way at a time. Bound by memory: 32768 x 8 slots x 4096 bfloat16 423 us, 5.7 TB/s.
 template <class T, int V, int G, int U, int A>
 __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
   using P = Piece<T, V>;
@@ -389,7 +396,8 @@ __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
 }
 
 // dR[place[t][c]] = w[t][c] X[t] and dw[t][c] = X[t] . R[place[t][c]], X the gradient of
-// k_combine's sum. A group of lanes has a whole token, A slots and U pieces of each at a time.
+// k_combine's sum. A group of lanes has a whole token, A slots and U pieces of each at a time: 16384
+// x 8 slots x 4096 bfloat16 438 us, 5.2 TB/s of reads and writes of rows in no order.
 template <class T, int V, int G, int U, int A>
 __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
   using P = Piece<T, V>;

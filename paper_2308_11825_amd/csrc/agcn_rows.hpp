@@ -101,18 +101,19 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // that wait for each other. GRAD: the kernel also keeps two sums a column and does best with a
 // row in as few lanes as its registers allow. us on one MI355X of layer_norm with residual and
 // of its gradients: 60,000 x 608 float16 59 in 64 lanes of 2 pieces and 63 in 32 of 3 (60 and 61);
-// 50,000 x 2048 bfloat16 134 in 128 of 2, 167 in 64 of 4, 140 in 256 of 1 (198, 143, 176); 16384 x
-// 4096 91 in 256 of 2, 97 in 512 of 1 (105 and 121); 32768 x 8192 381 in 512 of 2, 393 in 1024
-// of 1, 411 in 256 of 4 (395, 396, 360). Rows of 16 and 32 values in 4 and 8 lanes: 400,000 x 64
+// 50,000 x 2048 bfloat16 134 in 128 of 2, 167 in 64 of 4, 140 in 256 of 1 (198, 143, 176); 57,522 x
+// 2432 209 in 64 of 5, 241 in 128 of 3, 285 in 512 of 1 (240, 331, 254); 16384 x 4096 91 in 256 of 2, 97 in
+// 512 of 1 (105 and 121); 20,000 x 5120 153 in 256 of 3, 160 in 512 of 2 (177, and 169 in 256 of 4); 32768 x
+// 8192 381 in 512 of 2, 393 in 1024 of 1, 411 in 256 of 4 (395, 396, 360). Rows of 16 and 32 values in 4 and 8 lanes: 400,000 x 64
 // bfloat16 38, and 54 in 16 lanes. Calls use(Shape), or returns false for rows that are too long.
 template <int G, int NV>
 struct Shape {
   static constexpr int kG = G, kNV = NV;
 };
 constexpr int row_threads(int g) { return g > 64 ? g : 256; }  // of a workgroup
-template <bool SHORT, bool GRAD, class F>  // SHORT: 8 pieces at most
+template <int V, bool GRAD, class F>  // V: columns of a piece; 1 for rows of less than a piece
 bool row_shape(int64_t pieces, F use) {
-  if constexpr (SHORT) {
+  if constexpr (V == 1) {
     use(Shape<8, 1>{});
   } else {
     if (pieces <= 4) use(Shape<4, 1>{});
@@ -125,10 +126,23 @@ bool row_shape(int64_t pieces, F use) {
     else if (pieces <= 128) use(Shape<64, 2>{});
     else if (pieces <= 192) use(Shape<64, 3>{});
     else if (pieces <= 256) use(std::conditional_t<GRAD, Shape<64, 4>, Shape<128, 2>>{});
+    else if (pieces <= 320) use(Shape<64, 5>{});
+    else if (pieces <= 384) use(std::conditional_t<GRAD, Shape<256, 2>, Shape<128, 3>>{});
     else if (pieces <= 512) use(Shape<256, 2>{});
+    else if (pieces <= 768) use(Shape<256, 3>{});
     else if (pieces <= 1024) use(std::conditional_t<GRAD, Shape<256, 4>, Shape<512, 2>>{});
-    else if (pieces <= 2048) use(Shape<1024, 2>{});
-    else return false;
+    else if (pieces <= 1536) use(std::conditional_t<GRAD, Shape<1024, 2>, Shape<512, 3>>{});
+    else if (pieces <= 2048) use(std::conditional_t<GRAD, Shape<1024, 2>, Shape<512, 4>>{});
+    else if (pieces <= 3 * 1024) use(Shape<1024, 3>{});
+    else {
+      if constexpr (!GRAD || V <= 4) {  // (no registers for two sums of 32 columns)
+        if (pieces <= 4096) {
+          use(Shape<1024, 4>{});
+          return true;
+        }
+      }
+      return false;
+    }
   }
   return true;
 }

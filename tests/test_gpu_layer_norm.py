@@ -1,7 +1,7 @@
 """Layer norm and its gradients against the formulas in 64 bits.
 
-u = 2^-24. A lane adds V NV <= 24 values of a row one after the other (1024 threads f / 1024
-of a long one), and at most 16 more steps join the lanes: D = max(24, f / 1024) + 16
+u = 2^-24. A lane adds V NV <= 40 values of a row one after the other (1024 threads f / 1024
+of a long one), and at most 16 more steps join the lanes: D = max(40, f / 1024) + 16
 additions deep. A difference to the pivot, and then to the mean, is off by u of itself, the
 mean by D u times the mean size of the differences, which the row's 1 / sqrt(var + eps) brings to
 1 at most; that factor is off by D / 2 + 8 u of itself. So the normalised value is off by
@@ -20,7 +20,7 @@ EPS = 1e-5
 
 
 def depth(f):
-    return max(24, -(-f // 1024)) + 16
+    return max(40, -(-f // 1024)) + 16
 
 
 def check_norm(y, stats, h, g, b, dtype, eps=EPS):
@@ -53,9 +53,9 @@ def check_grad(got, dy, h, stats, g, dh, dtype, p_dtype):
     off = off + U * want.abs()
     off = off + half_step(dtype) * (want.abs() + off) + tiniest(dtype)
     assert bool(((dx.double() - want).abs() <= off).all()), ((dx.double() - want).abs() / off).max()
-    # Rows: a lane's own one after the other (1024 workgroups), 16 rows of a workgroup, the
-    # workgroups' sums 32 apart and then 32.
-    R = -(-n // 64) + 96 if f > 8192 else n // 1024 + 96
+    # Rows: a lane's own one after the other (256 workgroups or more; of long rows every 25th or more),
+    # 16 rows of a workgroup, the workgroups' sums 32 apart and then 32.
+    R = n // (25 if f > 8192 else 256) + 96
     for a, w, size in ((dg, want_g, (dy.double() * xh).abs().sum(0)), (db, want_b, dy.double().abs().sum(0))):
         off = U * (R + 4) * size
         off = off + half_step(p_dtype) * (w.abs() + off) + tiniest(p_dtype)
@@ -72,8 +72,8 @@ def inputs(n, f, dtype, p_dtype, *seed):
 
 # Every shape of lanes and pieces, both sides of each border, and rows past the registers.
 WIDTHS = [1, 2, 3, 4, 7, 8, 9, 15, 16, 63, 64, 65, 127, 128, 129, 192, 193, 255, 256, 257, 300, 384, 385,
-          512, 513, 601, 768, 769, 1000, 1024, 1025, 1536, 1537, 2048, 2049, 4096, 4097, 8191, 8192, 8193,
-          16384, 16385, 40001]
+          512, 513, 601, 768, 769, 1000, 1024, 1025, 1536, 1537, 2048, 2049, 2432, 2561, 3000, 3080, 4096, 4097, 5120, 6145, 8191, 8192,
+          8193, 10112, 12289, 16384, 16385, 20480, 24577, 32768, 32769, 40001]
 
 
 @pytest.mark.parametrize("dtype,p_dtype", [("float32", "float32"), ("bfloat16", "float32"), ("bfloat16", "bfloat16"),

@@ -148,3 +148,104 @@ def test_on_another_stream():
     assert torch.equal(out, want)
     again = agcn.combine_backward(x, z, place, w)
     assert torch.equal(dz, again[0]) and torch.equal(dw, again[1])
+
+
+def test_sorts_in_graphs():
+    """Two captured sorts of many slots, with workspaces, replayed in turn with other ids."""
+    cases = [(20000, 4, 50), (3000, 2, 3000), (300, 3, 12)]
+    ids = [torch.randint(-1, e + 1, (n, k), generator=gen(n, e), device=DEV).int() for n, k, e in cases]
+    graphs = []
+    for x, (n, k, e) in zip(ids, cases):
+        agcn.sort_groups(x, e)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = agcn.sort_groups(x, e)
+        graphs.append((graph, out))
+    for i in range(4):
+        for x, (n, k, e) in zip(ids, cases):
+            x.copy_(torch.randint(-1, e + 1, (n, k), generator=gen(n, e, i), device=DEV))
+        for graph, _ in graphs:
+            graph.replay()
+        for (_, out), x, (n, k, e) in zip(graphs, ids, cases):
+            want = agcn.sort_groups(x, e)
+            assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams at a time, each with workspaces of its own."""
+    n, f = 3000, 512
+    x = [randn((n, f), torch.bfloat16, s) for s in (1, 2)]
+    ids = [torch.randint(0, 40, (n, 6), generator=gen(s), device=DEV).int() for s in (1, 2)]
+    g = torch.ones(f, device=DEV)
+
+    def step(i, stream=None):
+        y, stats = agcn.layer_norm(x[i], g, stats=True, stream=stream)
+        grads = agcn.layer_norm_backward(y, x[i], stats, g, stream=stream)
+        offsets, place = agcn.sort_groups(ids[i], 40, stream=stream)
+        rows = agcn.dispatch(y, place, stream=stream)
+        return (y, stats, *grads, offsets, place, rows, agcn.combine(rows, place, stream=stream))
+
+    want = [step(0), step(1)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[step(i, s) for i, s in enumerate(streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for a, b in zip(pair, want):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_python_refuses_what_does_not_fit():
+    """Types, shapes, strides and devices, before anything runs; the C call's refusals as its error."""
+    x, g, s = torch.zeros((6, 8), device=DEV), torch.ones(8, device=DEV), torch.zeros((6, 2), device=DEV)
+    ids = torch.zeros((6, 2), dtype=torch.int32, device=DEV)
+    off, place = agcn.sort_groups(ids, 3)
+    R, w = torch.zeros((12, 8), device=DEV), torch.ones((6, 2), device=DEV)
+    Q, S = agcn.quantize_int(x)
+    WQ, WS = agcn.quantize_weight_int(torch.ones((8, 5), device=DEV))
+    WQ3, WS3 = agcn.quantize_weight_int(torch.ones((2, 8, 5), device=DEV))
+    offs = torch.zeros(3, dtype=torch.int32, device=DEV)
+    wrong_type = [
+        lambda: agcn.layer_norm(x.double(), g), lambda: agcn.layer_norm(x, g.half()), lambda: agcn.layer_norm(x, g.cpu()),
+        lambda: agcn.layer_norm(x, g, g.bfloat16()), lambda: agcn.layer_norm(x, g, residual=x.half()),
+        lambda: agcn.layer_norm(x, g, out=x.half()), lambda: agcn.layer_norm(x, None),
+        lambda: agcn.layer_norm_backward(x, x.half(), s, g), lambda: agcn.layer_norm_backward(x, x, s.double(), g),
+        lambda: agcn.sort_groups(ids.short(), 3), lambda: agcn.sort_groups(ids, 3, out=off),
+        lambda: agcn.sort_groups(ids, "3"), lambda: agcn.dispatch(x, place.long()), lambda: agcn.combine(R, place.long()),
+        lambda: agcn.combine(R.int(), place), lambda: agcn.combine(R, place, w.half()),
+        lambda: agcn.combine_backward(x.half(), R, place, w), lambda: agcn.combine_backward(x, R, place, None),
+        lambda: agcn.quantize_int(x.int()), lambda: agcn.int_linear(Q.float(), S, WQ, WS),
+        lambda: agcn.int_linear(Q, S.double(), WQ, WS), lambda: agcn.int_linear(Q, S, WQ, WS, dtype=torch.int32),
+        lambda: agcn.int_linear(Q, S, WQ, WS, dtype="float32"), lambda: agcn.int_linear(Q, S, WQ, WS.cpu()),
+        lambda: agcn.int_linear(Q, S, WQ, WS, dtype=torch.float16, out=torch.zeros((6, 5), device=DEV)),
+        lambda: agcn.grouped_int_linear(Q, S, WQ3, WS3, offs.long())]
+    for call in wrong_type:
+        with pytest.raises(TypeError):
+            call()
+    wrong_value = [
+        lambda: agcn.layer_norm(x[0], g), lambda: agcn.layer_norm(x, g[:7]), lambda: agcn.layer_norm(x, g, g[:7]),
+        lambda: agcn.layer_norm(x, g, hidden=x), lambda: agcn.layer_norm(x.t(), torch.ones(6, device=DEV)),
+        lambda: agcn.layer_norm(x, torch.ones(16, device=DEV)[::2]), lambda: agcn.layer_norm(x, g, residual=x[:5]),
+        lambda: agcn.layer_norm(x[:, :0], g[:0], stats=True), lambda: agcn.layer_norm_backward(x, x[:5], s, g),
+        lambda: agcn.layer_norm_backward(x, x, s[:, :1], g), lambda: agcn.sort_groups(ids[0], 3),
+        lambda: agcn.sort_groups(ids, -1), lambda: agcn.sort_groups(ids, 3, out=(off[:3], place)),
+        lambda: agcn.dispatch(x, place[:5]), lambda: agcn.dispatch(x, place[0]), lambda: agcn.dispatch(x, place, out=x),
+        lambda: agcn.combine(R[:11], place), lambda: agcn.combine(R, place, w[:, :1]),
+        lambda: agcn.combine_backward(x[:5], R, place, w), lambda: agcn.int_linear(Q, S[:5], WQ, WS),
+        lambda: agcn.int_linear(Q[:, :7], S, WQ, WS), lambda: agcn.int_linear(Q, S, WQ, WS, act="gelu"),
+        lambda: agcn.int_linear(Q, S, WQ3, WS3), lambda: agcn.grouped_int_linear(Q, S, WQ, WS, offs),
+        lambda: agcn.grouped_int_linear(Q, S, WQ3, WS3, offs[:2])]
+    for call in wrong_value:
+        with pytest.raises(ValueError):
+            call()
+    for call, status in ((lambda: agcn.layer_norm(x, g, eps=0.0), agcn.AGCN_ERR_INVALID_ARGUMENT),
+                         (lambda: agcn.layer_norm(x, g, out=x), agcn.AGCN_ERR_INVALID_ARGUMENT),
+                         (lambda: agcn.sort_groups(ids, 65537), agcn.AGCN_ERR_UNSUPPORTED),
+                         (lambda: agcn.combine(R[:, :0].expand(12, 0), place, out=torch.zeros((6, 0), device=DEV)), None)):
+        if status is None:
+            call()
+            continue
+        with pytest.raises(agcn.AgcnError) as e:
+            call()
+        assert e.value.status == status and agcn.agcn_last_error() in str(e.value)
