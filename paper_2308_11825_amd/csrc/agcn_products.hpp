@@ -1064,6 +1064,13 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
     // Few rows a group: bound by the weights, which are read once per row tile. 512 x 4096
     // -> 2048 over 64 groups 93 with 32 x 32 outputs, 99 with 64 x 64; 2048 rows 151, 117 and
     // 130 in k_qlinear_ring<32>; 4096 rows 236, 159 and 148.
+    // A short k has too few blocks for each wave to have its own: 64 x 512 -> 4096 over 64 groups 36 with
+    // 32 x 32 outputs, 21 with 64 x 64 and 20 in k_qlinear_tile's 64 x 64; 153 x 128 -> 8560 over 122 100,
+    // 57, 59 and x 512 170, 95, 117; 2000 x 256 -> 2048 over 64 40, 23, 13; 512 x 1024 -> 4096 53, 51, 51. (Integer
+    // sums are the same in any order.)
+    if (P == kInteger && rows < 64 && p.fin < (rows <= 12 ? 512 : 1024))
+      return launch_tile<32, 32, 2, 2, P, TY, GROUPED, true>(p, st);
+    if (P == kInteger && fits_y && rows < 64 && p.fin < 1024) return launch_stream<4, 4, 4, 1, P, TY, true>(p, st);
     if (fits_y && rows <= 12) return launch_stream<2, 2, 4, 2, P, TY, true>(p, st);
     if (fits_y && rows < 64) return launch_stream<4, 4, 4, 1, P, TY, true>(p, st);
   } else if (tiles(64, 64) <= kUnits) {
