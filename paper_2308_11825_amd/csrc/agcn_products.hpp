@@ -1048,14 +1048,23 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
     return m * ceil_div64(p.fout, bn);
   };
   if (!near || !async) {
-    if (fits_y && (!near || rows <= 64)) {
+    // Integer sums are the same in any order: the kernel by the workgroups alone. One a compute
+    // unit, two where k is short or each has 16 rows, hide k_qlinear_thin's loads better than the
+    // tile's; more only read more often. In 16 rows, in 32, and in 64 x 64 outputs: 8 x 4099 -> 4099 18, 23
+    // and 26; 32 rows 33, 33 and 26, 64 rows 56, 48 and 25; 64 x 1001 -> 1001 8.0, 9.1 and 11.2; 500 x 4097 -> 500 59,
+    // 45 and 24; 3719 x 7823 -> 17 45, 36 and 51; 5000 x 602 -> 41 over 7 groups 7.9 in 32, 12.5 in the last;
+    // 1000 x 1000 -> 1000 over 64 groups 41, 40 and 18, 64 x 2050 -> 1025 50, 62 and 29.
+    if (P == kInteger && near) {
+      const int64_t columns = ceil_div64(p.fout, 16);
+      if (fits_y && rows <= 64 && few_rows_grid(p.n, p.groups, 16, GROUPED) * columns <= 2 * kUnits)
+        return launch_thin<1, 4, P, TY, GROUPED>(p, st);
+      if (fits_y && few_rows_grid(p.n, p.groups, 32, GROUPED) * columns <= (p.fin < 1024 ? 2 : 1) * kUnits)
+        return launch_thin<2, 2, P, TY, GROUPED>(p, st);
+      if (rows <= 64) return launch_tile<32, 32, 2, 2, P, TY, GROUPED, false>(p, st);
+    } else if (fits_y && (!near || rows <= 64)) {
       if (rows <= 16) return launch_thin<1, 4, P, TY, GROUPED>(p, st);
       return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     }
-    // Few outputs and no rows to stage: the k of an output over eight waves. 5000 x 602 -> 41 over
-    // 7 groups 7.9 us, 12.5 in 64 x 64 tiles. (Integer sums are the same in any order.)
-    if (P == kInteger && fits_y && few_rows_grid(p.n, p.groups, 32, GROUPED) * ceil_div64(p.fout, 16) <= 4 * kUnits)
-      return launch_thin<2, 2, P, TY, GROUPED>(p, st);
     if (!near) return fail(AGCN_ERR_UNSUPPORTED, "row strides over 8 million bytes and over 65535 row tiles");
     if (tiles(64, 64) <= 4 * kUnits) return launch_tile<32, 32, 2, 2, P, TY, GROUPED, false>(p, st);
     return launch_tile<32, 64, 4, 1, P, TY, GROUPED, false>(p, st);

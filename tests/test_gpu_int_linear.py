@@ -185,6 +185,35 @@ def test_groups(n, fin, fout, sizes, first, dtype):
         assert not y[:first].any() and not y[int(off[-1]):].any()
 
 
+@pytest.mark.parametrize("n,groups,fin,fout", [(20, 64, 130, 300), (60, 40, 500, 70), (60, 40, 512, 1030), (700, 30, 96, 257),
+                                               (700, 30, 1000, 515), (700, 30, 1040, 64), (9, 3, 4099, 41), (33, 1, 2050, 4100),
+                                               (2000, 33, 640, 128), (40, 1, 300, 50)])
+def test_few_rows_of_a_group(n, groups, fin, fout):
+    """Short and long rows, on 16 bytes and not: the same sums; some groups have no rows, one most."""
+    ids = torch.randint(0, groups, (n // 2,), generator=gen(n, groups), device=DEV) // 2
+    sizes = torch.bincount(ids, minlength=groups)
+    sizes[groups // 2] += n - n // 2 - 2
+    off = offsets_of(sizes.tolist(), n, 1)
+    q, wq = ints((n, fin), 1), ints((groups, fout, fin), 2)
+    s, ws = torch.rand(n, device=DEV), torch.rand((groups, fout), device=DEV)
+    to = -(-fin // 16) * 16
+    rows, weights = (torch.full((*v.shape[:-1], to), 99, dtype=torch.int8, device=DEV)[..., :fin] for v in (q, wq))
+    rows.copy_(q), weights.copy_(wq)
+    y = agcn.grouped_int_linear(rows, s, weights, ws, off)
+    for i in range(groups):
+        a, b = int(off[i]), int(off[i + 1])
+        if b > a:
+            check(y[a:b], q[a:b], s[a:b], wq[i], ws[i])
+    assert not y[0].any() and not y[int(off[-1]):].any()
+    odd = padded(wq.view(-1, fin), 1, 1).unflatten(0, (groups, fout))
+    assert torch.equal(agcn.grouped_int_linear(padded(q, 1, 1), s, odd, ws, off), y)
+    for bad in (off.flip(0).contiguous(), off * 1000 - 700, off - 5):
+        raw = torch.full((n + 2, fout), 7.0, device=DEV)
+        agcn.grouped_int_linear(rows, s, weights, ws, bad, out=raw[1:-1])
+        agcn.grouped_int_linear(q, s, wq, ws, bad, out=raw[1:-1])
+        assert raw[0].eq(7).all() and raw[-1].eq(7).all()
+
+
 def test_offsets_that_break_the_rules_stay_inside():
     n, fin, fout = 300, 128, 64
     q, wq, s, ws = ints((n, fin), 1), ints((3, fout, fin), 2), torch.rand(n, device=DEV), torch.rand((3, fout), device=DEV)
