@@ -471,20 +471,51 @@ __global__ __launch_bounds__(row_threads(G)) void k_layer_norm_grad(GradArgs a) 
   }
 }
 
-// Rows too long for registers: dx, one workgroup a row.
+// V columns of a row from `at` on, `valid` of them its own.
+template <class T, int V>
+__device__ __forceinline__ void load_columns(float (&to)[V], const T* row, int at, int valid) {
+  if (valid == V) {
+    const auto v = load_any<Piece<T, V>>(row + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = to_float(v.e[i]);
+  } else {
+    for (int i = 0; i < V; ++i) to[i] = i < valid ? to_float(row[at + i]) : 0.0f;
+  }
+}
+
+// Rows too long for registers: dx, one workgroup a row (with the sums below 8000 x 30720 bfloat16 883
+// us, 1190 by single elements),
 template <class T>
 __global__ __launch_bounds__(1024) void k_layer_norm_grad_long(GradArgs a) {
+  constexpr int V = kPiece<T>;
   __shared__ float part[2][16];
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const T* dy = static_cast<const T*>(a.dY) + row * a.lddy;
     const T* h = static_cast<const T*>(a.H) + row * a.ldh;
     const Normalised norm(a.stats + row * a.lds);
+    auto each = [&](auto use) {
+      for (int c = threadIdx.x * V; c < a.f; c += 1024 * V) {
+        const int valid = min(V, a.f - c);
+        float y[V], x[V], g[V];
+        load_columns(y, dy, c, valid);
+        load_columns(x, h, c, valid);
+        if (valid == V) {
+          load_params<T>(g, a.g, c, a.p_float);
+        } else {
+          for (int i = 0; i < V; ++i) g[i] = i < valid ? load_param<T>(a.g, c + i, a.p_float) : 0.0f;
+        }
+        use(c, valid, y, x, g);
+      }
+    };
     float s1 = 0.0f, s2 = 0.0f;
-    for (int c = threadIdx.x; c < a.f; c += 1024) {
-      const float d = to_float(dy[c]) * load_param<T>(a.g, c, a.p_float);
-      s1 += d;
-      s2 = fmaf(d, norm(to_float(h[c])), s2);
-    }
+    each([&](int, int valid, const float(&y)[V], const float(&x)[V], const float(&g)[V]) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = y[i] * g[i];
+        s1 += i < valid ? d : 0.0f;
+        s2 += i < valid ? d * norm(x[i]) : 0.0f;
+      }
+    });
     s1 = lanes_sum<64>(s1);
     s2 = lanes_sum<64>(s2);
     __syncthreads();  // the row before has been read
@@ -496,28 +527,48 @@ __global__ __launch_bounds__(1024) void k_layer_norm_grad_long(GradArgs a) {
     const float over = 1.0f / (float)a.f;
     s1 = sum16(part[0][threadIdx.x % 16]) * over;
     s2 = sum16(part[1][threadIdx.x % 16]) * over;
-    for (int c = threadIdx.x; c < a.f; c += 1024) {
-      float d = norm.rs * (fmaf(to_float(dy[c]), load_param<T>(a.g, c, a.p_float), -s1) - norm(to_float(h[c])) * s2);
-      if (a.dH != nullptr) d += to_float(static_cast<const T*>(a.dH)[row * a.lddh + c]);
-      static_cast<T*>(a.dX)[row * a.lddx + c] = (T)d;
-    }
+    each([&](int c, int valid, const float(&y)[V], const float(&x)[V], const float(&g)[V]) {
+      float dh[V] = {};
+      if (a.dH != nullptr) load_columns(dh, static_cast<const T*>(a.dH) + row * a.lddh, c, valid);
+      T* to = static_cast<T*>(a.dX) + row * a.lddx + c;
+      Piece<T, V> o;
+#pragma unroll
+      for (int i = 0; i < V; ++i) o.e[i] = (T)(norm.rs * (fmaf(y[i], g[i], -s1) - norm(x[i]) * s2) + dh[i]);
+      if (valid == V) {
+        store_any(to, o);
+      } else {
+        for (int i = 0; i < valid; ++i) to[i] = o.e[i];
+      }
+    });
   }
 }
-// and the columns' sums, a thread a column over every gridDim.y-th row.
+// and the columns' sums, a thread V columns over every gridDim.y-th row.
 template <class T>
 __global__ __launch_bounds__(256) void k_layer_norm_columns(GradArgs a) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
+  constexpr int V = kPiece<T>;
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
   if (c >= a.f) return;
-  float dg = 0.0f, db = 0.0f;
+  const int valid = (int)std::min<int64_t>(V, a.f - c);
+  float dg[V] = {}, db[V] = {};
+#pragma unroll 2
   for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
     const Normalised norm(a.stats + row * a.lds);
-    const float y = to_float(static_cast<const T*>(a.dY)[row * a.lddy + c]);
-    dg = fmaf(y, norm(to_float(static_cast<const T*>(a.H)[row * a.ldh + c])), dg);
-    db += y;
+    float y[V], x[V];
+    load_columns(y, static_cast<const T*>(a.dY) + row * a.lddy, (int)c, valid);
+    load_columns(x, static_cast<const T*>(a.H) + row * a.ldh, (int)c, valid);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      dg[i] = fmaf(y[i], norm(x[i]), dg[i]);
+      db[i] += y[i];
+    }
   }
-  float* to = a.part + (int64_t)blockIdx.y * 2 * a.f;
-  to[c] = dg;
-  to[a.f + c] = db;
+  float* to = a.part + (int64_t)blockIdx.y * 2 * a.f + c;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < valid) {
+      to[i] = dg[i];
+      to[a.f + i] = db[i];
+    }
 }
 
 // Column sums of `parts` rows of 2 f values: 32 columns a workgroup, every 32nd row a
@@ -593,7 +644,7 @@ int64_t grad_groups(int64_t n, int32_t f, int64_t v) {
   const int64_t pieces = ceil_div64(f, v);
   if (v == 1 ? row_shape<1, true>(pieces, set) : v == 4 ? row_shape<4, true>(pieces, set) : row_shape<8, true>(pieces, set))
     return groups;
-  return std::min<int64_t>(n, std::max<int64_t>(1, 2048 / ceil_div64(f, 256)));
+  return std::min<int64_t>(n, std::max<int64_t>(1, 1024 * v / ceil_div64(f, 256)));
 }
 
 template <class T>
@@ -618,7 +669,7 @@ int grad_pieces(const GradArgs& a, void* dg, void* db, hipStream_t st) {
     k_layer_norm_grad_long<T><<<(unsigned)std::min(kLongRowGroups, a.n), 1024, 0, st>>>(a);
     if (int rc = launched("k_layer_norm_grad_long launch")) return rc;
     if (a.part != nullptr)
-      k_layer_norm_columns<T><<<dim3((unsigned)ceil_div64(a.f, 256), (unsigned)groups), 256, 0, st>>>(a);
+      k_layer_norm_columns<T><<<dim3((unsigned)ceil_div64(a.f, 256 * kPiece<T>), (unsigned)groups), 256, 0, st>>>(a);
   }
   if (int rc = launched("k_layer_norm_grad launch")) return rc;
   if (a.part == nullptr) return AGCN_OK;

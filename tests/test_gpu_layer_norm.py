@@ -92,7 +92,8 @@ def test_every_width(f, dtype, p_dtype):
 
 
 @pytest.mark.parametrize("n,f,dtype", [(5000, 128, "float32"), (40000, 41, "bfloat16"), (3000, 601, "float16"),
-                                       (1500, 4096, "bfloat16"), (2500, 1024, "float32"), (100, 20000, "bfloat16")])
+                                       (1500, 4096, "bfloat16"), (2500, 1024, "float32"), (100, 20000, "bfloat16"),
+                                       (300, 33001, "float16"), (200, 17001, "float32")])
 def test_many_rows_without_residual_or_bias(n, f, dtype):
     dtype = TYPES[dtype]
     x, _, g, _ = inputs(n, f, dtype, torch.float32)
