@@ -850,6 +850,8 @@ def _call_native(name, stream, *args):
     native = _native or _load_native()
     if stream is None:
         return getattr(native, name)(*args)
+    if isinstance(args[0], _torch.Tensor) and args[0].is_cuda and args[0].device != stream.device:
+        raise ValueError(f"stream must be one of {args[0].device}, as the tensors are")
     with _torch.cuda.stream(stream):
         results = getattr(native, name)(*args)
     for t in args:
@@ -864,7 +866,11 @@ def _load_native():
     lib = load_library()
     if _torch is None:
         _load_torch()
-    from . import _binding
+    try:
+        from . import _binding
+    except ImportError as e:
+        raise ImportError(f"the compiled binding is missing or does not fit this PyTorch ({e}): build it with "
+                          "`python -m paper_2308_11825_amd.build`") from e
     _binding.init(AgcnError, [ctypes.cast(getattr(lib, "agcn_" + n), _vp).value for n in _NATIVE])
     _native = _binding
     return _native

@@ -65,10 +65,17 @@ def build(verbose: bool = False) -> str:
     return LIB_PATH
 
 
-def build_binding(verbose: bool = False) -> str:
-    """Compile _binding.so against the installed PyTorch. It takes the library's functions by
-    their addresses, so the two can be built in any order."""
-    import torch
+def build_binding(verbose: bool = False) -> str | None:
+    """Compile _binding.so against the installed PyTorch; without one built for ROCm there is
+    none to build, and libagcn.so serves C callers. It takes the library's functions by their
+    addresses, so the two can be built in any order."""
+    try:
+        import torch
+    except ImportError:
+        torch = None
+    if torch is None or torch.version.hip is None:
+        print("no PyTorch for ROCm: libagcn.so without its compiled Python binding", flush=True)
+        return None
     top = os.path.dirname(torch.__file__)
     lib = os.path.join(top, "lib")
     tmp = BINDING_PATH + ".tmp"

@@ -171,6 +171,17 @@ def test_sorts_in_graphs():
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
 
 
+def test_a_stream_of_another_device_is_refused():
+    class Elsewhere:
+        device = torch.device("cuda", torch.cuda.device_count())
+
+    x, ids = torch.randn(5, 64, device=DEV), torch.zeros((5, 1), dtype=torch.int64, device=DEV)
+    for call in (lambda s: agcn.layer_norm(x, x[0], stream=s), lambda s: agcn.sort_groups(ids, 3, stream=s),
+                 lambda s: agcn.quantize_int(x, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(Elsewhere())
+
+
 def test_two_streams_at_once():
     """The same calls on two streams at a time, each with workspaces of its own."""
     n, f = 3000, 512
