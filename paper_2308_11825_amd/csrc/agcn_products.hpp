@@ -1082,6 +1082,10 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
     if (P == kInteger && fits_y && rows < 64 && p.fin < 1024) return launch_stream<4, 4, 4, 1, P, TY, true>(p, st);
     if (fits_y && rows <= 12) return launch_stream<2, 2, 4, 2, P, TY, true>(p, st);
     if (fits_y && rows < 64) return launch_stream<4, 4, 4, 1, P, TY, true>(p, st);
+    // Few outputs and a long k, which only k_qlinear_stream splits: 332 x 9728 -> 651 over 4 groups 22 with
+    // 32 x 32 outputs, 40 in 64 x 64 tiles, 32 in k_qlinear_ring<32>; 1000 x 2048 -> 128 4.8, 7.9, 11.0.
+    if (P == kInteger && fits_y && p.fin >= 2048 && tiles(32, 32) <= kUnits)
+      return launch_stream<2, 2, 4, 2, P, TY, true>(p, st);
   } else if (tiles(64, 64) <= kUnits) {
     // Few outputs: the largest tile of which there are not more than compute units, each
     // read by a workgroup that splits k over its waves. 16, 64, 128 and 256 x 4096 -> 4096:
@@ -1115,8 +1119,10 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
   // conversions do. ring<32> and the smaller tile: 512 x 4096 -> 4096 21.5 and 23.4
   // (k_qlinear_stream); 1024 x 2048 -> 2048 11.6 and 12.8 (64 x 64); 16384 x 512 -> 512 10.8 and 13.0 (128 x
   // 64); 4096 x 1024 -> 1024 9.2 and 11.3. float32: 512 x 4096 -> 4096 33.4 and 25.6 (stream), 1024 x 2048
-  // -> 2048 19.4 and 15.6.
-  if (p.fout > 64 && tiles(128, 128) >= (P == kExact ? kUnits : kUnits / 2))
+  // -> 2048 19.4 and 15.6. Groups of integers with a long k, for which k_qlinear_tile is what is left: 5386 x
+  // 10112 -> 128 over 10 33 and 41, 5000 x 4096 -> 128 over 40 17.5 and 19.5; 1660 x 3584 -> 141 over 5 16.5 and 11.2.
+  if (p.fout > 64 && (tiles(128, 128) >= (P == kExact ? kUnits : kUnits / 2) ||
+                      (P == kInteger && GROUPED && p.fin >= 4096)))
     return launch_ring<32, P, TY, GROUPED>(p, st);
   // Two workgroups a compute unit, each wave with blocks of its own.
   if constexpr (!GROUPED)

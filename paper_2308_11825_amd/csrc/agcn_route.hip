@@ -299,6 +299,11 @@ struct Slot {
   }
 };
 
+// Few tokens: a token's columns (k_combine_grad: slots) over gridDim.y workgroups, `each` of them
+// a workgroup and turn.
+__device__ __forceinline__ int64_t part_start(int first, int each) { return first + (int64_t)blockIdx.y * each; }
+__device__ __forceinline__ int64_t part_step(int each) { return (int64_t)gridDim.y * each; }
+
 // The token of a group of G lanes: one for the whole wave in scalar registers.
 template <int G>
 __device__ __forceinline__ int64_t token_of(int64_t i) {
@@ -323,7 +328,7 @@ __global__ __launch_bounds__(256) void k_dispatch(RowArgs a) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
     const uint8_t* x = static_cast<const uint8_t*>(a.X) + t * a.ldx;
-    for (int64_t at = lane * W; at < a.f; at += G * W * U) {
+    for (int64_t at = part_start(lane, G * U) * W; at < a.f; at += part_step(G * U) * W) {
       Bytes<W> v[U];
       int64_t from[U];
 #pragma unroll
@@ -354,7 +359,7 @@ __global__ __launch_bounds__(256) void k_combine(RowArgs a) {
   for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
-    for (int64_t at = lane * V; at < a.f; at += G * V * U) {
+    for (int64_t at = part_start(lane, G * U) * V; at < a.f; at += part_step(G * U) * V) {
       int64_t from[U];
       float sum[U][V];
 #pragma unroll
@@ -405,13 +410,13 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
   for (int64_t i = xcd_tile(blockIdx.x, gridDim.x); i * (256 / G) < a.n; i += gridDim.x) {
     const int64_t t = token_of<G>(i);
     if (t >= a.n) continue;
-    for (int c0 = 0; c0 < a.k; c0 += A) {
+    for (int64_t c0 = part_start(0, A); c0 < a.k; c0 += part_step(A)) {
       int64_t row[A];
       float w[A], dot[A];
       bool kept[A], inside[A];
 #pragma unroll
       for (int u = 0; u < A; ++u) {
-        const int c = min(c0 + u, a.k - 1);
+        const int c = (int)std::min<int64_t>(c0 + u, a.k - 1);
         const Slot s(a, t, c);
         row[u] = s.row;
         kept[u] = s.kept;
@@ -458,8 +463,11 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowArgs a) {
 // Workgroups of a launch, at most; rows past them are looped over.
 constexpr int64_t kMostGroups = 1 << 20;
 template <int G>
-unsigned row_grid(int64_t n) {
-  return (unsigned)std::min<int64_t>(kMostGroups, ceil_div64(n, 256 / G));
+dim3 row_grid(int64_t n, int64_t parts) {
+  const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(kMostGroups, ceil_div64(n, 256 / G)));
+  // Up to four workgroups a compute unit: k_combine of 200 x 8 slots x 8192 bfloat16 6.8 us, 9.6 with a
+  // workgroup a token; k_combine_grad 22 and 37, of 48 x 8 x 4096 9.5 and 16.5; k_dispatch 6.0 and 7.0.
+  return dim3((unsigned)groups, (unsigned)std::max<int64_t>(1, std::min<int64_t>(parts, 1024 / groups)));
 }
 
 int bits_of(int bins) {
@@ -544,12 +552,12 @@ int combine_pieces(const RowArgs& a, hipStream_t st) {
     constexpr int A = decltype(at_once)::value;
     // Rows over 4 KB: the lanes of four waves, two pieces each.
     if (V > 1 && pieces > 256) {
-      k_combine<T, V, 256, 2, A><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+      k_combine<T, V, 256, 2, A><<<row_grid<256>(a.n, ceil_div64(pieces, 512)), 256, 0, st>>>(a);
       return;
     }
     token_shape<V == 1>(pieces, [&](auto shape) {
       constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
-      k_combine<T, V, G, U, A><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+      k_combine<T, V, G, U, A><<<row_grid<G>(a.n, ceil_div64(pieces, G * U)), 256, 0, st>>>(a);
     });
   });
   return launched("k_combine launch");
@@ -560,7 +568,7 @@ int combine_grad_pieces(const RowArgs& a, hipStream_t st) {
     constexpr int A = decltype(at_once)::value;
     token_shape<V == 1>(ceil_div64(a.f, V), [&](auto shape) {
       constexpr int G = decltype(shape)::kG, U = decltype(shape)::kNV;
-      k_combine_grad<T, V, G, U, A><<<row_grid<G>(a.n), 256, 0, st>>>(a);
+      k_combine_grad<T, V, G, U, A><<<row_grid<G>(a.n, ceil_div64(a.k, A)), 256, 0, st>>>(a);
     });
   });
   return launched("k_combine_grad launch");
@@ -581,12 +589,12 @@ int combine_any(const RowArgs& a, int32_t dtype, bool grad, hipStream_t st) {
 template <int W>
 int dispatch_pieces(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = ceil_div64(a.f, W);
-  if (pieces <= 1) k_dispatch<W, 1, 1><<<row_grid<1>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 4) k_dispatch<W, 4, 1><<<row_grid<4>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 16 || W < 16) k_dispatch<W, 16, 1><<<row_grid<16>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 64) k_dispatch<W, 64, 1><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else if (pieces <= 128) k_dispatch<W, 64, 2><<<row_grid<64>(a.n), 256, 0, st>>>(a);
-  else k_dispatch<W, 256, 2><<<row_grid<256>(a.n), 256, 0, st>>>(a);
+  if (pieces <= 1) k_dispatch<W, 1, 1><<<row_grid<1>(a.n, ceil_div64(pieces, 1)), 256, 0, st>>>(a);
+  else if (pieces <= 4) k_dispatch<W, 4, 1><<<row_grid<4>(a.n, ceil_div64(pieces, 4)), 256, 0, st>>>(a);
+  else if (pieces <= 16 || W < 16) k_dispatch<W, 16, 1><<<row_grid<16>(a.n, ceil_div64(pieces, 16)), 256, 0, st>>>(a);
+  else if (pieces <= 64) k_dispatch<W, 64, 1><<<row_grid<64>(a.n, ceil_div64(pieces, 64)), 256, 0, st>>>(a);
+  else if (pieces <= 128) k_dispatch<W, 64, 2><<<row_grid<64>(a.n, ceil_div64(pieces, 128)), 256, 0, st>>>(a);
+  else k_dispatch<W, 256, 2><<<row_grid<256>(a.n, ceil_div64(pieces, 512)), 256, 0, st>>>(a);
   return launched("k_dispatch launch");
 }
 
