@@ -420,6 +420,12 @@ def _call(device, fn, *args):
         return fn(*args)
 
 
+def _written_out(name, t):
+    """Refuses a lazily negated view (of the imaginary part of a conjugate): its memory is not its values."""
+    if t.is_neg():
+        raise TypeError(f"{name} must not be a lazily negated view: resolve_neg() writes it out")
+
+
 def _unit_col_stride(t):
     return t.shape[1] <= 1 or t.shape[0] == 0 or t.stride(1) == 1
 
@@ -446,6 +452,7 @@ class Plan:
                 raise TypeError(f"{name} must be a CUDA tensor of dtype {dt}")
             if t.dim() != 1 or not t.is_contiguous():
                 raise ValueError(f"{name} must be 1-D and contiguous")
+            _written_out(name, t)
         self.device = rowptr.device
         self.n_rows = rowptr.numel() - 1
         self.n_cols = self.n_rows if n_cols is None else int(n_cols)
@@ -511,6 +518,7 @@ class Plan:
             raise TypeError("X must be a float32 tensor on the plan's device")
         if X.dim() != 2 or X.shape[0] != self.n_cols or not _unit_col_stride(X):
             raise ValueError("X must be (n_cols, F) with unit column stride")
+        _written_out("X", X)
         F = X.shape[1]
         if F < 1:
             raise ValueError("F must be >= 1")
@@ -519,6 +527,7 @@ class Plan:
         if (tuple(out.shape) != (self.n_rows, F) or not _unit_col_stride(out)
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, F) tensor with unit column stride")
+        _written_out("out", out)
         if ws is None:
             ws = self.workspace(F, stream)
         st = stream.cuda_stream if stream is not None else _stream_handle(self.device)
@@ -535,6 +544,7 @@ class Plan:
                     or t.dtype != torch.float32 or t.dim() != 2 or not _unit_col_stride(t)):
                 raise TypeError(f"{name} must be a 2-D float32 tensor on the plan's device with "
                                 "unit column stride")
+            _written_out(name, t)
         fin, fout = W.shape
         if X.shape != (self.n_cols, fin):
             raise ValueError("X must be (n_cols, fin) with fin = W.shape[0]")
@@ -543,6 +553,7 @@ class Plan:
         if (tuple(out.shape) != (self.n_rows, fout) or not _unit_col_stride(out)
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, fout) tensor with unit column stride")
+        _written_out("out", out)
         if ws is None:
             nb = agcn_gcn_workspace_size(self.handle, fout)
             if stream is None:
@@ -592,6 +603,7 @@ def linear(X, W, out=None, stream=None):
         if (not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dtype != torch.float32
                 or t.dim() != 2 or not _unit_col_stride(t)):
             raise TypeError(f"{name} must be a 2-D float32 CUDA tensor with unit column stride")
+        _written_out(name, t)
     n, fin = X.shape
     if W.shape[0] != fin or W.device != X.device:
         raise ValueError("W must be (fin, fout) on X's device")
@@ -600,6 +612,7 @@ def linear(X, W, out=None, stream=None):
         out = torch.empty((n, fout), dtype=torch.float32, device=X.device)
     if tuple(out.shape) != (n, fout) or not _unit_col_stride(out) or out.dtype != torch.float32:
         raise ValueError("out must be a float32 (n, fout) tensor with unit column stride")
+    _written_out("out", out)
     st = stream.cuda_stream if stream is not None else _stream_handle(X.device)
     _call(X.device, agcn_linear, n, fin, fout, X.data_ptr(), _row_stride(X), W.data_ptr(),
           _row_stride(W), out.data_ptr(), _row_stride(out), st)
@@ -633,6 +646,8 @@ def _matrix(name, t, device, shape, dtype):
     tensor has: these checks are the larger part of a small call's time.)"""
     if isinstance(t, _torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device:
         stride = t.stride()
+        if t.is_neg():
+            _written_out(name, t)
         if stride[-1] == 1 and shape[-2] > 1:
             return stride[-2]
         if shape[-1] <= 1 or t.numel() == 0 or stride[-1] == 1:
@@ -752,6 +767,7 @@ def rms_norm(X, weight, residual=None, eps=1e-6, hidden=None, out=None, stream=N
         raise TypeError("weight must be float32 or of X's type")
     if weight.shape != (f,) or (f > 1 and weight.stride(0) != 1):
         raise ValueError("weight must be (f,) and contiguous")
+    _written_out("weight", weight)
     r = h = None
     ldr = ldh = 0
     if residual is not None:
@@ -808,6 +824,7 @@ def _product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
         raise TypeError("offsets must be int32 on the inputs' device")
     if offsets.shape != (groups + 1,) or (groups > 0 and offsets.stride(0) != 1):
         raise ValueError("offsets must be (groups + 1,) and contiguous")
+    _written_out("offsets", offsets)
     _call(device, agcn_grouped_linear, n, fin, fout, groups, Q.data_ptr(), ldq, S.data_ptr(), lds,
           WQ.data_ptr(), ldwq, WQ.stride(0), WS.data_ptr(), ldws, WS.stride(0), offsets.data_ptr(),
           code, out.data_ptr(), ldy, st, epilogue)

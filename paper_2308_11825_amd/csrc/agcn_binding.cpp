@@ -73,9 +73,13 @@ std::string text(at::IntArrayRef shape) {
 const Tensor& tensor(const std::string& name, PyObject* o, at::Device device) {
   if (!THPVariable_Check(o) || THPVariable_Unpack(o).device() != device)
     type_error(name + " must be a tensor on " + device.str());
-  return THPVariable_Unpack(o);
+  const Tensor& t = THPVariable_Unpack(o);
+  // The memory of such a view is not its values.
+  if (t.is_conj()) type_error(name + " must not be a lazily conjugated view: resolve_conj() writes it out");
+  if (t.is_neg()) type_error(name + " must not be a lazily negated view: resolve_neg() writes it out");
+  return t;
 }
-// The tensor that sets a call's sizes and type.
+// The tensor that sets a call's sizes and type; matrix() checks the rest of it.
 const Tensor& first(const std::string& name, PyObject* o, int64_t dims, bool weight = false) {
   if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) type_error(name + " must be a CUDA tensor");
   const Tensor& t = THPVariable_Unpack(o);
