@@ -410,6 +410,16 @@ def _stream_handle(device):
     return raw(device.index)
 
 
+def _handle_of(stream, device):
+    """Handle of the stream that the caller chose, or of torch's current one. Nothing orders
+    a stream of another device with the tensors."""
+    if stream is None:
+        return _stream_handle(device)
+    if stream.device != device:
+        raise ValueError(f"stream must be one of {device}, as the tensors are")
+    return stream.cuda_stream
+
+
 def _call(device, fn, *args):
     """fn(*args) with `device` current (the context only where it is not)."""
     import torch
@@ -469,7 +479,7 @@ class Plan:
         prm.flags = flags
         self.params = prm
         self._handle = None
-        st = stream.cuda_stream if stream is not None else _stream_handle(self.device)
+        st = _handle_of(stream, self.device)
         self._handle = _call(self.device, agcn_plan_create, self.n_rows, self.n_cols, self.nnz,
                              rowptr.data_ptr(), colidx.data_ptr() if self.nnz else None,
                              vals.data_ptr() if self.nnz else None, prm, st)
@@ -501,7 +511,7 @@ class Plan:
             nb = self._ws_bytes[F] = self.workspace_bytes(F)
         if nb == 0:
             return None
-        key = (F, stream.cuda_stream if stream is not None else _stream_handle(self.device))
+        key = (F, _handle_of(stream, self.device))
         ws = self._ws.get(key)
         if ws is None:
             # allocated on the stream that uses it, so torch's allocator orders
@@ -528,9 +538,9 @@ class Plan:
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, F) tensor with unit column stride")
         _written_out("out", out)
+        st = _handle_of(stream, self.device)
         if ws is None:
             ws = self.workspace(F, stream)
-        st = stream.cuda_stream if stream is not None else _stream_handle(self.device)
         _call(self.device, agcn_spmm_ex, self.handle, F, X.data_ptr(), _row_stride(X),
               out.data_ptr(), _row_stride(out), ws.data_ptr() if ws is not None else None, st,
               _EPILOGUES[act])
@@ -554,6 +564,7 @@ class Plan:
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, fout) tensor with unit column stride")
         _written_out("out", out)
+        st = _handle_of(stream, self.device)
         if ws is None:
             nb = agcn_gcn_workspace_size(self.handle, fout)
             if stream is None:
@@ -561,7 +572,6 @@ class Plan:
             else:
                 with torch.cuda.stream(stream):
                     ws = torch.empty((nb + 3) // 4, dtype=torch.float32, device=self.device)
-        st = stream.cuda_stream if stream is not None else _stream_handle(self.device)
         _call(self.device, agcn_gcn_layer, self.handle, fin, fout, X.data_ptr(), _row_stride(X),
               W.data_ptr(), _row_stride(W), out.data_ptr(), _row_stride(out), ws.data_ptr(), st,
               _EPILOGUES[act])
@@ -613,7 +623,7 @@ def linear(X, W, out=None, stream=None):
     if tuple(out.shape) != (n, fout) or not _unit_col_stride(out) or out.dtype != torch.float32:
         raise ValueError("out must be a float32 (n, fout) tensor with unit column stride")
     _written_out("out", out)
-    st = stream.cuda_stream if stream is not None else _stream_handle(X.device)
+    st = _handle_of(stream, X.device)
     _call(X.device, agcn_linear, n, fin, fout, X.data_ptr(), _row_stride(X), W.data_ptr(),
           _row_stride(W), out.data_ptr(), _row_stride(out), st)
     return out
@@ -686,18 +696,19 @@ def _dtype_code(name, dtype):
 def _on_stream(device, stream, tensors):
     """The stream's handle; on a stream of the caller's choice torch's allocator must
     not reuse the tensors' memory before its work."""
-    if stream is None:
-        return _stream_handle(device)
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return stream.cuda_stream
+    st = _handle_of(stream, device)
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return st
 
 
 def _new(like, stream, shape, dtype):
     """A tensor on like's device, allocated on the stream that writes it."""
     if stream is None:
         return like.new_empty(shape, dtype=dtype)
+    _handle_of(stream, like.device)
     with _torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
 
@@ -867,8 +878,8 @@ def _call_native(name, stream, *args):
     native = _native or _load_native()
     if stream is None:
         return getattr(native, name)(*args)
-    if isinstance(args[0], _torch.Tensor) and args[0].is_cuda and args[0].device != stream.device:
-        raise ValueError(f"stream must be one of {args[0].device}, as the tensors are")
+    if isinstance(args[0], _torch.Tensor) and args[0].is_cuda:
+        _handle_of(stream, args[0].device)
     with _torch.cuda.stream(stream):
         results = getattr(native, name)(*args)
     for t in args:

@@ -1,0 +1,35 @@
+"""Calls of the routed layer's operators that are refused or fail, and how they say so."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_2308_11825_amd as agcn  # noqa: E402
+from routed_helpers import randn  # noqa: E402
+
+DEV = "cuda:0"
+
+
+class Elsewhere:
+    """A stream of a device that the tensors are not on."""
+    device = torch.device("cuda", 1)
+    cuda_stream = 0
+
+
+def test_a_stream_of_another_device_is_refused_by_every_function():
+    n, f = 6, 32
+    x, g, W = randn((n, f), torch.float32, 1), randn((f,), torch.float32, 2), randn((f, 8), torch.float32, 3)
+    s = Elsewhere()
+    Q, S = agcn.quantize(x)
+    WQ, WS = agcn.quantize_weight(W)
+    rowptr, colidx, vals = torch.arange(n + 1, device=DEV).int(), torch.arange(n, device=DEV).int(), g[:n].clone()
+    plan = agcn.Plan(rowptr, colidx, vals)
+    offsets = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    for call in (lambda: agcn.quantize_weight_int(W, stream=s), lambda: agcn.quantize_weight(W, stream=s),
+                 lambda: agcn.quantize(x, stream=s), lambda: agcn.quantize(x, out=(Q, S), stream=s),
+                 lambda: agcn.rms_norm(x, g, stream=s), lambda: agcn.quantized_linear(Q, S, WQ, WS, stream=s),
+                 lambda: agcn.grouped_linear(Q, S, WQ[None], WS[None], offsets, stream=s),
+                 lambda: agcn.linear(x, W, stream=s), lambda: agcn.Plan(rowptr, colidx, vals, stream=s),
+                 lambda: plan.spmm(x, stream=s), lambda: plan.gcn_layer(x, W, stream=s)):
+        with pytest.raises(ValueError, match="stream must be one of cuda:0"):
+            call()
