@@ -899,7 +899,8 @@ def _load_native():
     except ImportError as e:
         raise ImportError(f"the compiled binding is missing or does not fit this PyTorch ({e}): build it with "
                           "`python -m paper_2308_11825_amd.build`") from e
-    _binding.init(AgcnError, [ctypes.cast(getattr(lib, "agcn_" + n), _vp).value for n in _NATIVE])
+    _binding.init(AgcnError, _torch.OutOfMemoryError,
+                  [ctypes.cast(getattr(lib, "agcn_" + n), _vp).value for n in _NATIVE])
     _native = _binding
     return _native
 

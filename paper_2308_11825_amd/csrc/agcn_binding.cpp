@@ -43,7 +43,7 @@ struct Library {
   decltype(&agcn_grouped_int_linear) grouped_int_linear;
   decltype(&agcn_last_error) last_error;
 } lib;
-PyObject* agcn_error = nullptr;
+PyObject *agcn_error = nullptr, *memory_error = nullptr;  // the package's, and torch's where its allocator fails
 
 // A Python exception to raise.
 struct Refused {
@@ -427,17 +427,22 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
       Py_DECREF(e);
     }
   } catch (const c10::OutOfMemoryError& e) {
-    PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
+    PyErr_SetString(memory_error, e.what_without_backtrace());
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   }
   return nullptr;
 }
 
-// init(AgcnError, addresses): the addresses of Library's functions in its order.
+void keep(PyObject*& to, PyObject* o) {
+  Py_INCREF(o);
+  Py_XDECREF(to);
+  to = o;
+}
+// init(AgcnError, torch.OutOfMemoryError, addresses): the addresses of Library's functions in its order.
 PyObject* init(PyObject*, PyObject* args) {
-  PyObject *error, *list;
-  if (!PyArg_ParseTuple(args, "OO!", &error, &PyList_Type, &list)) return nullptr;
+  PyObject *error, *memory, *list;
+  if (!PyArg_ParseTuple(args, "OOO!", &error, &memory, &PyList_Type, &list)) return nullptr;
   constexpr Py_ssize_t kCount = sizeof(Library) / sizeof(void*);
   if (PyList_GET_SIZE(list) != kCount) {
     PyErr_SetString(PyExc_ValueError, "wrong number of addresses");
@@ -452,9 +457,8 @@ PyObject* init(PyObject*, PyObject* args) {
     }
   }
   memcpy(static_cast<void*>(&lib), to, sizeof(lib));
-  Py_INCREF(error);
-  Py_XDECREF(agcn_error);
-  agcn_error = error;
+  keep(agcn_error, error);
+  keep(memory_error, memory);
   Py_RETURN_NONE;
 }
 

@@ -33,3 +33,23 @@ def test_a_stream_of_another_device_is_refused_by_every_function():
                  lambda: plan.spmm(x, stream=s), lambda: plan.gcn_layer(x, W, stream=s)):
         with pytest.raises(ValueError, match="stream must be one of cuda:0"):
             call()
+
+
+def test_memory_that_runs_out_is_torchs_error():
+    """The same exception from all functions, whichever of them allocates."""
+    x = randn((1000, 1024), torch.float32, 1)
+    _, place = agcn.sort_groups(torch.zeros((1000, 256), dtype=torch.int32, device=DEV), 1)
+    W = torch.zeros((1, 1024), device=DEV).expand(1024, 1024).contiguous()
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    try:
+        # What is held now and 256 MB more: the allocator itself refuses the gigabyte of results.
+        torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + 2 ** 28) / total)
+        with pytest.raises(torch.OutOfMemoryError):
+            x.new_empty((256000, 1024))
+        with pytest.raises(torch.OutOfMemoryError) as e:
+            agcn.dispatch(x, place)
+        assert isinstance(e.value, RuntimeError) and "memory" in str(e.value)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert agcn.dispatch(x, place).shape == (256000, 1024) and agcn.quantize_weight_int(W)[0].shape == (1024, 1024)
