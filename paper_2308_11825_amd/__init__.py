@@ -663,7 +663,7 @@ def _matrix(name, t, device, shape, dtype):
         if shape[-1] <= 1 or t.numel() == 0 or stride[-1] == 1:
             # Any value >= a row is valid for 0 or 1 rows.
             return stride[-2] if shape[-2] > 1 else max(shape[-1], stride[-2])
-        raise ValueError(f"{name} must have unit column stride")
+        raise ValueError(f"{name} must have unit column stride, as its contiguous() has")
     if not isinstance(t, _torch.Tensor) or t.device != device:
         raise TypeError(f"{name} must be a tensor on {device}")
     if t.dtype is not dtype:
@@ -969,7 +969,9 @@ def layer_norm_backward(grad, H, stats, weight, bias=True, grad_hidden=None, out
     """Gradients of ``layer_norm`` from grad, that of y: (dX, dweight, dbias). H: the rows h (X
     where there was no residual); stats: as ``layer_norm`` gave them; grad_hidden: the gradient
     of h from elsewhere, added to dX, which is that of X and of the residual; bias=False: dbias
-    is None; out: where dX is written. dweight and dbias have weight's type."""
+    is None; out: where dX is written. dweight and dbias have weight's type. (An expanded
+    gradient, as that of a sum, is refused: its contiguous() copy will do, here and in
+    ``combine_backward``.)"""
     return _call_native("layer_norm_backward", stream, grad, H, stats, weight, bias, grad_hidden, out)
 
 

@@ -103,7 +103,10 @@ Matrix matrix(const std::string& name, PyObject* o, at::Device device, at::IntAr
   const Tensor& t = tensor(name, o, device);
   same(name, t, shape, dtype);
   const int64_t rows = shape[shape.size() - 2], columns = shape.back();
-  if (columns > 1 && t.numel() > 0 && t.stride(-1) != 1) value_error(name + " must have unit column stride");
+  if (columns > 1 && t.numel() > 0 && t.stride(-1) != 1)
+    value_error(name + " must have unit column stride, as its contiguous() has");
+  if (rows > 1 && t.numel() > 0 && t.stride(-2) < columns)
+    value_error(name + " must have rows that do not overlap, as its contiguous() has");
   // Any value >= a row is valid for 0 or 1 rows.
   return {&t, rows > 1 && t.numel() > 0 ? t.stride(-2) : std::max(columns, t.stride(-2))};
 }

@@ -53,3 +53,21 @@ def test_memory_that_runs_out_is_torchs_error():
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert agcn.dispatch(x, place).shape == (256000, 1024) and agcn.quantize_weight_int(W)[0].shape == (1024, 1024)
+
+
+def test_expanded_gradients_are_refused_with_the_way_out():
+    """The gradient of a sum has strides of 0: what to do about it is said."""
+    n, k, f = 6, 2, 16
+    x, g, w = randn((n, f), torch.float32, 1), randn((f,), torch.float32, 2), randn((n, k), torch.float32, 3)
+    _, stats = agcn.layer_norm(x, g, stats=True)
+    _, place = agcn.sort_groups(torch.zeros((n, k), dtype=torch.int32, device=DEV), 1)
+    R = agcn.dispatch(x, place)
+    for grad in (torch.ones((), device=DEV).expand(n, f), torch.ones(f, device=DEV).expand(n, f),
+                 torch.ones((n, 1), device=DEV).expand(n, f), randn((f, n), torch.float32, 4).t()):
+        for call in (lambda grad: agcn.layer_norm_backward(grad, x, stats, g), lambda grad: agcn.layer_norm(grad, g),
+                     lambda grad: agcn.combine_backward(grad, R, place, w), lambda grad: agcn.quantize_int(grad)):
+            with pytest.raises(ValueError, match=r"contiguous\(\)"):
+                call(grad)
+            call(grad.contiguous())
+    with pytest.raises(ValueError, match=r"contiguous\(\)"):
+        agcn.combine(R, place, torch.ones(k, device=DEV).expand(n, k))
