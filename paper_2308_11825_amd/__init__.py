@@ -714,9 +714,10 @@ def _new(like, stream, shape, dtype):
 
 
 def _new_rows(like, stream, lead, k, dtype=None):
-    """Values (..., k) in 8 bits (e4m3 unless told otherwise) and their row stride: rows start on 16 bytes, on 128 (the
-    lines of memory, which a block of 128 columns then is one of) where that adds an
-    eighth at most: 230,000 x 602 -> 256 bfloat16 78 us with rows of 640 bytes, 83 with 608."""
+    """Values (..., k) in 8 bits (e4m3 unless told otherwise) and their row stride: rows
+    start on 16 bytes, on 128 (the lines of memory, which a block of 128 columns then is one
+    of) where that adds an eighth at most: 230,000 x 602 -> 256 bfloat16 78 us with rows of 640
+    bytes, 83 with 608."""
     ld = (k + 127) // 128 * 128
     if ld > k + k // 8:
         ld = (k + 15) // 16 * 16
@@ -988,15 +989,17 @@ def sort_groups(ids, groups, out=None, stream=None):
 
 def dispatch(X, place, out=None, stream=None):
     """The rows of X (n, f), of any type, in group order: (n * k, f) with row place[t][c] = X[t],
-    and rows of ids without a group 0. Its gradient is ``combine`` of the rows' without
-    weights."""
+    and rows of ids without a group 0. Rows of one-byte types start on 16 bytes or 128, as
+    ``quantize_int`` lays them: a view of wider rows. The gradient of ``dispatch`` is ``combine`` of the
+    rows' without weights (none is recorded)."""
     return _call_native("dispatch", stream, X, place, out)
 
 
 def combine(R, place, weights=None, out=None, stream=None):
     """(n, f) with row t the sum over c of weights[t][c] R[place[t][c]], ids without a group left
     out: R (n * k, f) float32, bfloat16 or float16 rows in group order, place (n, k) as
-    ``sort_groups`` gives it, weights (n, k) float32 or None (all 1). Added in 32 bits."""
+    ``sort_groups`` gives it, weights (n, k) float32 or None (all 1). Added in 32 bits. No gradient is
+    recorded: ``combine_backward`` gives it."""
     return _call_native("combine", stream, R, place, weights, out)
 
 

@@ -5,9 +5,10 @@
 // rounded once to fp32 and once by each scale.
 //
 // The kernels are those of agcn_products.hpp with the matrix cores' integer instructions, as many
-// cycles as the e4m3 ones. Where the matrix cores bound them, power does: 16384 x 8192 -> 8192 874 to 975 us, 2.3
-// to 2.5 POP/s, with the matrix cores at work in 66 % of the cycles of a clock that falls to 1.6 GHz;
-// 32768 x 4096 -> 2048 258 us, and 241 for zeros. 1 x 4096 -> 4096 4.7 us.
+// cycles as the e4m3 ones. Where the matrix cores bound them, power does: 16384 x 8192 -> 8192 818 to 900 us, 2.4
+// to 2.7 POP/s, with the matrix cores at work in 77 % of the cycles of a clock that falls to 1.6 GHz;
+// 32768 x 4096 -> 2048 with one weight 248 us, and 168 for zeros. 1 x 4096 -> 4096 4.9 us, 3.4 TB/s of
+// weights: 128 workgroups of 32 columns, which leave half of the compute units without loads.
 #include "agcn_products.hpp"
 
 namespace agcn {

@@ -158,7 +158,7 @@ __device__ __forceinline__ void block_products(Sum4<P> (&acc)[NT][MT], GetW w, G
 // its column's. Sums that nothing was added to are 0 whatever the scales. A thread asks for
 // the scales of one row and one column of the tile before the products and passes them on
 // through LDS after them: asked for where they are needed, they cost a 256 x 256 tile 32 loads one
-// after the other (32768 x 4096 -> 2048 288 us, and 258 this way).
+// after the other (32768 x 4096 -> 2048 with one weight 288 us, and 258 this way).
 template <Products P>
 struct Scales {
   float row = 0.0f, column = 0.0f;
@@ -1052,7 +1052,10 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
     // unit, two where k is short or each has 16 rows, hide k_qlinear_thin's loads better than the
     // tile's; more only read more often. In 16 rows, in 32, and in 64 x 64 outputs: 8 x 4099 -> 4099 18, 23
     // and 26; 32 rows 33, 33 and 26, 64 rows 56, 48 and 25; 64 x 1001 -> 1001 8.0, 9.1 and 11.2; 500 x 4097 -> 500 59,
-    // 45 and 24; 3719 x 7823 -> 17 45, 36 and 51; 5000 x 602 -> 41 over 7 groups 7.9 in 32, 12.5 in the last;
+    // 45 and 24; 3719 x 7823 -> 17 45, 36 and 51; 5000 x 602 -> 41 over 7 groups 7.9 in 32, 12.5 in the last.
+    // With one to two workgroups a compute unit, in 32 rows and in the last: 500 x 301 -> 500 8.4 and 9.2, x 601 9.2 and
+    // 9.9, x 999 10.8 and 11.2, x 1201 11.3 and 10.9, x 2001 16.7 and 14.5, and within 5 % of these 200 x ... -> 1000,
+    // 7000 x ... -> 30 and 4900 x ... -> 33 over 7;
     // 1000 x 1000 -> 1000 over 64 groups 41, 40 and 18, 64 x 2050 -> 1025 50, 62 and 29.
     if (P == kInteger && near) {
       const int64_t columns = ceil_div64(p.fout, 16);
@@ -1121,6 +1124,9 @@ int linear_typed(const LinearArgs& p, hipStream_t st) {
   // 64); 4096 x 1024 -> 1024 9.2 and 11.3. float32: 512 x 4096 -> 4096 33.4 and 25.6 (stream), 1024 x 2048
   // -> 2048 19.4 and 15.6. Groups of integers with a long k, for which k_qlinear_tile is what is left: 5386 x
   // 10112 -> 128 over 10 33 and 41, 5000 x 4096 -> 128 over 40 17.5 and 19.5; 1660 x 3584 -> 141 over 5 16.5 and 11.2.
+  // With few tiles too: 560 x 8192 -> 512 over 8 28.0 and 33.8, 512 x 8192 -> 512 over 4 27.0 and 34.5 (32 and 24 tiles of 128 x
+  // 128); at the bound itself fewer than about 64 tiles lose as often as they gain (560 x 4096 -> 512 over 8 17.0 and
+  // 12.4, 1024 x 4096 -> 512 over 8 16.7 and 18.2), more gain a tenth.
   if (p.fout > 64 && (tiles(128, 128) >= (P == kExact ? kUnits : kUnits / 2) ||
                       (P == kInteger && GROUPED && p.fin >= 4096)))
     return launch_ring<32, P, TY, GROUPED>(p, st);

@@ -1,4 +1,4 @@
-// Shared by the 8-bit operators (agcn_quant.hip, agcn_qlinear.hip): element
+// Shared by the 8-bit operators (agcn_quant.hip, agcn_products.hpp) and agcn_rows.hpp: element
 // types, blocks, and the power-of-two scale of a block.
 #pragma once
 

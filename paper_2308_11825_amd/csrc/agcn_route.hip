@@ -465,8 +465,11 @@ constexpr int64_t kMostGroups = 1 << 20;
 template <int G>
 dim3 row_grid(int64_t n, int64_t parts) {
   const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(kMostGroups, ceil_div64(n, 256 / G)));
-  // Up to four workgroups a compute unit: k_combine of 200 x 8 slots x 8192 bfloat16 6.8 us, 9.6 with a
-  // workgroup a token; k_combine_grad 22 and 37, of 48 x 8 x 4096 9.5 and 16.5; k_dispatch 6.0 and 7.0.
+  // Up to four workgroups a compute unit, as far as a token has `parts`: a workgroup's pieces of its columns (512
+  // of 16 bytes where rows are over 4 KB: 48 x 4096 bfloat16 stay 48 workgroups) or, for k_combine_grad, A of its
+  // slots (two parts of 8). k_combine of 200 x 8 slots x 8192 bfloat16 6.8 us, 9.6 with a workgroup a token;
+  // k_combine_grad 22 and 37 (100 workgroups: four tokens each, in two parts), of 48 x 8 x 4096 9.5 and 16.5; k_dispatch
+  // 6.0 and 7.0.
   return dim3((unsigned)groups, (unsigned)std::max<int64_t>(1, std::min<int64_t>(parts, 1024 / groups)));
 }
 

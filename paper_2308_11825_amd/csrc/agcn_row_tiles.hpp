@@ -1,5 +1,5 @@
 // The rows of a matrix, or of its groups, cut into tiles, one workgroup each: which rows a
-// workgroup of agcn_qlinear.hip's kernels works on. The groups' offsets are device memory
+// workgroup of agcn_products.hpp's kernels works on. The groups' offsets are device memory
 // that the caller may fill with anything; whatever they hold, a tile lies inside the matrix.
 //
 // Needs HIP's device functions (hip_runtime.h) or, on the host, stand-ins for them.
