@@ -533,14 +533,14 @@ class Plan:
         if F < 1:
             raise ValueError("F must be >= 1")
         if out is None:
-            out = torch.empty((self.n_rows, F), dtype=torch.float32, device=self.device)
+            out = _new(X, stream, (self.n_rows, F), torch.float32)
         if (tuple(out.shape) != (self.n_rows, F) or not _unit_col_stride(out)
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, F) tensor with unit column stride")
         _written_out("out", out)
-        st = _handle_of(stream, self.device)
         if ws is None:
             ws = self.workspace(F, stream)
+        st = _on_stream(self.device, stream, (X, out, ws))
         _call(self.device, agcn_spmm_ex, self.handle, F, X.data_ptr(), _row_stride(X),
               out.data_ptr(), _row_stride(out), ws.data_ptr() if ws is not None else None, st,
               _EPILOGUES[act])
@@ -559,19 +559,15 @@ class Plan:
         if X.shape != (self.n_cols, fin):
             raise ValueError("X must be (n_cols, fin) with fin = W.shape[0]")
         if out is None:
-            out = torch.empty((self.n_rows, fout), dtype=torch.float32, device=self.device)
+            out = _new(X, stream, (self.n_rows, fout), torch.float32)
         if (tuple(out.shape) != (self.n_rows, fout) or not _unit_col_stride(out)
                 or out.dtype != torch.float32 or out.device != self.device):
             raise ValueError("out must be a float32 (n_rows, fout) tensor with unit column stride")
         _written_out("out", out)
-        st = _handle_of(stream, self.device)
         if ws is None:
             nb = agcn_gcn_workspace_size(self.handle, fout)
-            if stream is None:
-                ws = torch.empty((nb + 3) // 4, dtype=torch.float32, device=self.device)
-            else:
-                with torch.cuda.stream(stream):
-                    ws = torch.empty((nb + 3) // 4, dtype=torch.float32, device=self.device)
+            ws = _new(X, stream, ((nb + 3) // 4,), torch.float32)
+        st = _on_stream(self.device, stream, (X, W, out, ws))
         _call(self.device, agcn_gcn_layer, self.handle, fin, fout, X.data_ptr(), _row_stride(X),
               W.data_ptr(), _row_stride(W), out.data_ptr(), _row_stride(out), ws.data_ptr(), st,
               _EPILOGUES[act])
@@ -619,11 +615,11 @@ def linear(X, W, out=None, stream=None):
         raise ValueError("W must be (fin, fout) on X's device")
     fout = W.shape[1]
     if out is None:
-        out = torch.empty((n, fout), dtype=torch.float32, device=X.device)
+        out = _new(X, stream, (n, fout), torch.float32)
     if tuple(out.shape) != (n, fout) or not _unit_col_stride(out) or out.dtype != torch.float32:
         raise ValueError("out must be a float32 (n, fout) tensor with unit column stride")
     _written_out("out", out)
-    st = _handle_of(stream, X.device)
+    st = _on_stream(X.device, stream, (X, W, out))
     _call(X.device, agcn_linear, n, fin, fout, X.data_ptr(), _row_stride(X), W.data_ptr(),
           _row_stride(W), out.data_ptr(), _row_stride(out), st)
     return out
@@ -708,6 +704,8 @@ def _new(like, stream, shape, dtype):
     """A tensor on like's device, allocated on the stream that writes it."""
     if stream is None:
         return like.new_empty(shape, dtype=dtype)
+    if _torch is None:
+        _load_torch()
     _handle_of(stream, like.device)
     with _torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
