@@ -616,8 +616,9 @@ def linear(X, W, out=None, stream=None):
     fout = W.shape[1]
     if out is None:
         out = _new(X, stream, (n, fout), torch.float32)
-    if tuple(out.shape) != (n, fout) or not _unit_col_stride(out) or out.dtype != torch.float32:
-        raise ValueError("out must be a float32 (n, fout) tensor with unit column stride")
+    if (tuple(out.shape) != (n, fout) or not _unit_col_stride(out) or out.dtype != torch.float32
+            or out.device != X.device):
+        raise ValueError("out must be a float32 (n, fout) tensor with unit column stride on X's device")
     _written_out("out", out)
     st = _on_stream(X.device, stream, (X, W, out))
     _call(X.device, agcn_linear, n, fin, fout, X.data_ptr(), _row_stride(X), W.data_ptr(),

@@ -71,3 +71,10 @@ def test_expanded_gradients_are_refused_with_the_way_out():
             call(grad.contiguous())
     with pytest.raises(ValueError, match=r"contiguous\(\)"):
         agcn.combine(R, place, torch.ones(k, device=DEV).expand(n, k))
+
+
+def test_linear_refuses_an_out_that_is_not_on_its_device():
+    """(Its address would be written to by the kernel.)"""
+    x, W = randn((6, 8), torch.float32, 1), randn((8, 4), torch.float32, 2)
+    with pytest.raises(ValueError, match="device"):
+        agcn.linear(x, W, out=torch.zeros((6, 4)))
