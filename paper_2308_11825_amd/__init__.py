@@ -403,11 +403,11 @@ def _stream_handle(device):
     """Handle of torch's current stream on `device`: what
     torch.cuda.current_stream(device).cuda_stream is, without the Stream
     object (1.9 us of a call of 11; where torch has the raw query)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None or device.index is None:
-        return torch.cuda.current_stream(device).cuda_stream
-    return raw(device.index)
+    if _torch is None:
+        _load_torch()
+    if _raw_stream is None or device.index is None:
+        return _torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device.index)
 
 
 def _handle_of(stream, device):
@@ -422,11 +422,11 @@ def _handle_of(stream, device):
 
 def _call(device, fn, *args):
     """fn(*args) with `device` current (the context only where it is not)."""
-    import torch
-    current = getattr(torch._C, "_cuda_getDevice", None)
-    if current is not None and current() == device.index:
+    if _torch is None:
+        _load_torch()
+    if _current_device is not None and _current_device() == device.index:
         return fn(*args)
-    with torch.cuda.device(device):
+    with _torch.cuda.device(device):
         return fn(*args)
 
 
@@ -636,11 +636,14 @@ _MOST_INT32 = 2 ** 31 - 1
 _DTYPES = {}  # torch dtype -> AGCN_FLOAT, AGCN_BFLOAT, AGCN_HALF
 _torch = None
 _Q8 = _S8 = None  # the dtypes of values and of scales
+_raw_stream = _current_device = None  # torch's raw queries, where it has them
 
 
 def _load_torch():
-    global _torch, _Q8, _S8
+    global _torch, _Q8, _S8, _raw_stream, _current_device
     import torch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None)
     _DTYPES.update({torch.float32: AGCN_FLOAT, torch.bfloat16: AGCN_BFLOAT,
                     torch.float16: AGCN_HALF})
     _Q8, _S8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -693,11 +696,12 @@ def _dtype_code(name, dtype):
 def _on_stream(device, stream, tensors):
     """The stream's handle; on a stream of the caller's choice torch's allocator must
     not reuse the tensors' memory before its work."""
+    if stream is None:
+        return _stream_handle(device)
     st = _handle_of(stream, device)
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
     return st
 
 
@@ -778,7 +782,8 @@ def rms_norm(X, weight, residual=None, eps=1e-6, hidden=None, out=None, stream=N
         raise TypeError("weight must be float32 or of X's type")
     if weight.shape != (f,) or (f > 1 and weight.stride(0) != 1):
         raise ValueError("weight must be (f,) and contiguous")
-    _written_out("weight", weight)
+    if weight.is_neg():
+        _written_out("weight", weight)
     r = h = None
     ldr = ldh = 0
     if residual is not None:
@@ -835,7 +840,8 @@ def _product(Q, S, WQ, WS, offsets, dtype, act, out, stream):
         raise TypeError("offsets must be int32 on the inputs' device")
     if offsets.shape != (groups + 1,) or (groups > 0 and offsets.stride(0) != 1):
         raise ValueError("offsets must be (groups + 1,) and contiguous")
-    _written_out("offsets", offsets)
+    if offsets.is_neg():
+        _written_out("offsets", offsets)
     _call(device, agcn_grouped_linear, n, fin, fout, groups, Q.data_ptr(), ldq, S.data_ptr(), lds,
           WQ.data_ptr(), ldwq, WQ.stride(0), WS.data_ptr(), ldws, WS.stride(0), offsets.data_ptr(),
           code, out.data_ptr(), ldy, st, epilogue)
